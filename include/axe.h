@@ -323,6 +323,118 @@ int axe_gemm_grouped_pair_static(const axe_gemm_grouped_desc_t* g1, const axe_ge
                                  void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * What stands around the two group GEMMs of an MoE layer (Sec. 4.1, "fused MoE layer"): the norm in front of it, the router, the rows
+ * of the tokens in the experts' order, and the way back; each with its gradient.  T tokens, H columns, E experts, k experts per token;
+ * row (t, j) of the experts' order belongs to token t's j-th choice, M >= T k rows in all.
+ *
+ * Matrices carry layouts on `mem_axis` like the operands of axe_gemm: pitched, unit stride along the columns, no replicas, any offset and
+ * any pitch of at least the columns (16-byte multiples are not required; they are faster); *_elems are the buffers' sizes in elements.
+ * Everything else is contiguous and row-major.  T = 0 is a call without rows: the layouts are not looked at, axe_route writes
+ * group_rows = 0 and axe_rmsnorm_backward d_dweight = 0.
+ * Buffers are aligned to their elements and outputs are disjoint from the inputs and from each other (AXE_EINVAL), but for what is said below.
+ * Sums, norms and softmax statistics are held in 32 bits; results do not depend on how the work was split (no atomics on values), so a call
+ * repeats its bits.  Nothing is allocated; the calls may be captured into a graph. */
+
+/* axe_rmsnorm -- y = h rho(h) w,  h = x + residual,  rho(h) = (mean_c h_c^2 + eps)^(-1/2), row by row.
+ *   x, residual, sum : (T, H) of x_dtype (AXE_BF16, AXE_F16 or AXE_F32).  d_residual NULL: h = x.  d_sum (optional) receives h, rounded once; the norm
+ *       is taken of the unrounded h.  d_sum may be d_x or d_residual with the same layout.
+ *   d_w : H weights of weight_dtype (one of the same three), or NULL: ones.
+ *   y : (T, H) of y_dtype: x_dtype; AXE_BF16 or AXE_F16 of AXE_F32 rows; or AXE_FP8_E4M3 with d_scales row-major (T, ceil(H / 128)),
+ *       fp32 or E8M0 by scale_dtype, one scale per row and 128 columns, which is what axe_gemm (scale_a_rows = 1) and axe_gemm_grouped read:
+ *           q = e4m3(y / s), round to nearest even,   fp32: s = max(|y|) / 448, at least 2^-126;   E8M0: the smallest power of two not below
+ *           max(|y|) / 448, at least 2^-126;   s = 1 where all of the 128 are 0.
+ *       NaNs are left out of the maximum and stay NaN; an infinite maximum counts as the largest fp32 number, infinities become +-448.
+ *       (axe_gemm_grouped reads E8M0 codes in words: pad that allocation to a multiple of 4 bytes.)
+ *       d_y may be d_x or d_residual with the same layout and element size.
+ * H up to 32768 (else AXE_EUNSUPPORTED).
+ *
+ * axe_rmsnorm_backward -- the gradients, from h (d_sum of the forward call; `sum` is its layout) and dy (y_dtype, layout y; a quantised
+ * y passes its gradient in 16 bits: describe it as such):
+ *     dx = rho (w dy - h rho^2 mean_c(w dy h)) + dsum,      dw = sum_t dy h rho.
+ *   d_dsum : the gradient that arrives at h itself, layout `residual`, x_dtype, or NULL.  d_dx : layout x, the gradient of x and of residual alike; may be d_dsum or
+ *   d_dy with the same layout and element size.  d_dweight : H fp32, or NULL.
+ *   d_ws, ws_elems : workspace of axe_rmsnorm_workspace(g) 4-byte words (may be 0), owned by the caller; not needed without d_dweight. */
+typedef struct {
+  int64_t      T, H;
+  int32_t      x_dtype, y_dtype, weight_dtype;
+  int32_t      scale_dtype;              /* AXE_SCALE_F32 or AXE_SCALE_E8M0; with AXE_FP8_E4M3 only */
+  float        eps;
+  int32_t      mem_axis;
+  axe_layout_t x, residual, sum, y;      /* residual and sum are looked at when their buffers are given */
+  int64_t      x_elems, residual_elems, sum_elems, y_elems;
+} axe_rmsnorm_desc_t;
+
+int axe_rmsnorm(const axe_rmsnorm_desc_t* g, const void* d_x, const void* d_residual, const void* d_w, void* d_sum, void* d_y, void* d_scales,
+                void* stream);
+int axe_rmsnorm_backward(const axe_rmsnorm_desc_t* g, const void* d_dy, const void* d_sum, const void* d_w, const void* d_dsum, void* d_dx,
+                         float* d_dweight, int32_t* d_ws, int64_t ws_elems, void* stream);
+int64_t axe_rmsnorm_workspace(const axe_rmsnorm_desc_t* g);   /* words, or a negative error */
+
+/* axe_route -- top-k routing.  logits (T, E) of logit_dtype (AXE_F32, AXE_BF16, AXE_F16), E up to 1024, k up to 64 and at most E.
+ *     s = softmax(l) (AXE_ROUTE_SOFTMAX) or 1 / (1 + exp(-l)) (AXE_ROUTE_SIGMOID),      choice c_e = s_e + bias_e   (d_bias: E fp32 or NULL)
+ *   groups > 1: the E / groups consecutive experts of a group stand or fall together; a group's score is its largest choice
+ *   (AXE_ROUTE_GROUP_MAX) or the sum of its two largest (AXE_ROUTE_GROUP_TOP2), and the groups_kept best groups stay (groups up to 64, a divisor of E).
+ *   d_ids (T, k) int32: the k largest choices of what is left, largest first, equal ones lowest index first (experts and groups).
+ *   d_weights (T, k) fp32: scale * s of the chosen, divided by their sum if renorm (0 if that sum is 0).  The bias does not enter.
+ *   Masked experts: a logit of -inf or NaN, or a choice of -inf or NaN, is never chosen; its softmax score is 0.  A row with fewer than k experts left has id -1, weight 0
+ *   in the places that remain (all of them, if it leaves none).  The lowest finite value of a type is no mask: such experts come last.  +inf counts as the largest fp32 number.
+ *   Without bias, softmax choices are compared by their logits (the same order, no rounding).
+ *   The experts' order (both given or both NULL): d_group_rows (E + 1) int32, what axe_gemm_grouped reads: expert e has the rows group_rows[e] ..
+ *   group_rows[e+1]-1; d_row_of (T, k) int32: the row of (t, j), by expert, then token; -1 where the id is -1.  T k < 2^31.
+ *   d_ws, ws_elems : workspace of axe_route_workspace(g) 4-byte words (0 for small T), owned by the caller, overwritten; needed with the order only.
+ *
+ * axe_route_backward -- the gradient of the logits from that of the weights, ids taken as they are (entries outside [0, E): no choice):
+ *     dL/ds_e = (dL/dw_j scale, renorm: (dL/dw_j scale - sum_i dL/dw_i w_i) / sum_i s_i)  for e = ids_j, 0 elsewhere, then through the softmax or the sigmoid.
+ *   d_dlogits : (T, E) with the layout and type of logits (every element written; masked experts: 0), may be d_logits.  Renormalised softmax
+ *   weights depend on the chosen logits only: the others get 0. */
+enum { AXE_ROUTE_SOFTMAX = 0, AXE_ROUTE_SIGMOID = 1 };
+enum { AXE_ROUTE_GROUP_MAX = 0, AXE_ROUTE_GROUP_TOP2 = 1 };
+typedef struct {
+  int64_t      T;
+  int32_t      E, k;
+  int32_t      logit_dtype, score, renorm;
+  int32_t      groups, groups_kept, group_score;
+  float        scale;
+  int32_t      mem_axis;
+  axe_layout_t logits;
+  int64_t      logits_elems;
+  const float* d_bias;
+} axe_route_desc_t;
+
+int axe_route(const axe_route_desc_t* g, const void* d_logits, int32_t* d_ids, float* d_weights, int32_t* d_group_rows, int32_t* d_row_of,
+              int32_t* d_ws, int64_t ws_elems, void* stream);
+int axe_route_backward(const axe_route_desc_t* g, const void* d_logits, const int32_t* d_ids, const float* d_dweights, void* d_dlogits, void* stream);
+int64_t axe_route_workspace(const axe_route_desc_t* g);       /* words, or a negative error */
+
+/* axe_rows_* -- the tokens' rows in the experts' order and back.  tokens (T, H) of tokens_dtype, rows (M, H) of rows_dtype; d_row_of (T, k) int32 as axe_route writes it:
+ * entries outside [0, M) are no row, and no two entries name one row.
+ *
+ * axe_rows_dispatch -- rows[row_of[t][j]] = tokens[t].  Rows that no entry names are left as they are.  Types: equal (AXE_BF16, AXE_F16 or AXE_F32); rows in AXE_FP8_E4M3 from
+ *   tokens in one of those, quantised once per token as axe_rmsnorm does it, d_scales (M, ceil(H / 128)) by scale_dtype; or both AXE_FP8_E4M3, bytes and
+ *   scales copied (d_token_scales (T, ceil(H / 128))).  The gradient is axe_rows_combine without weights.
+ *   d_row_of NULL: the rows are in order already (k = 1, M = T): a quantiser of rows, e.g. between the two products of an fp8 layer.
+ * axe_rows_combine -- tokens[t] = add[t] + sum_j weights[t][j] rows[row_of[t][j]], in the order of j, in fp32, rounded once.  d_weights (T, k) fp32 or NULL
+ *   (ones); d_add (layout and type of tokens) or NULL, may be d_tokens.  A weight of 0 does not make a row absent (0 * inf is NaN); an entry that is no row does.
+ * axe_rows_combine_backward -- d_drows[row_of[t][j]] = weights[t][j] dtokens[t] (layout and type of rows; may be d_rows) and
+ *   d_dweights[t][j] = sum_c dtokens[t][c] rows[row_of[t][j]][c] (0 where there is no row).  Either output may be NULL; d_rows may be NULL without d_dweights.
+ * The last two: one type, AXE_BF16, AXE_F16 or AXE_F32.  k up to 64; H, M below 2^31. */
+typedef struct {
+  int64_t      T, M, H;
+  int32_t      k;
+  int32_t      tokens_dtype, rows_dtype, scale_dtype;
+  int32_t      mem_axis;
+  axe_layout_t tokens, rows;
+  int64_t      tokens_elems, rows_elems;
+} axe_rows_desc_t;
+
+int axe_rows_dispatch(const axe_rows_desc_t* g, const void* d_tokens, const void* d_token_scales, const int32_t* d_row_of, void* d_rows, void* d_scales,
+                      void* stream);
+int axe_rows_combine(const axe_rows_desc_t* g, const void* d_rows, const int32_t* d_row_of, const float* d_weights, const void* d_add, void* d_tokens,
+                     void* stream);
+int axe_rows_combine_backward(const axe_rows_desc_t* g, const void* d_dtokens, const void* d_rows, const int32_t* d_row_of, const float* d_weights,
+                              void* d_drows, float* d_dweights, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * axe_gemm_describe -- the Axe layouts of every tile movement of the kernel axe_gemm would
  * launch for `g` (Sec. 3.1 / Fig. 3: tensors in shared memory and registers carry layouts; tile
  * composes register tile (x) lane (x) wave (x) workgroup, Sec. 3.3).  Host only, no device work.

@@ -23,13 +23,17 @@ AXE_TILE_AUTO, AXE_TILE_64x64x32, AXE_TILE_256x256x64, AXE_TILE_256x224x64 = 0, 
 AXE_MAX_RANK = 8
 AXE_SCALE_F32, AXE_SCALE_E8M0 = 0, 1
 AXE_EPI_NONE, AXE_EPI_SWIGLU = 0, 1
+AXE_ROUTE_SOFTMAX, AXE_ROUTE_SIGMOID = 0, 1
+AXE_ROUTE_GROUP_MAX, AXE_ROUTE_GROUP_TOP2 = 0, 1
 AXE_GROUPED_AUTO, AXE_GROUPED_TILES, AXE_GROUPED_STREAM, AXE_GROUPED_TILES_256, AXE_GROUPED_TILES_128 = 0, 1, 2, 3, 4
 
 EXPORTS = ["axe_layout_eval", "axe_relayout", "axe_gemm", "axe_gemm_grouped", "axe_gemm_grouped_check", "axe_gemm_grouped_pair", "axe_gemm_grouped_pair_fused",
            "axe_gemm_grouped_pair_status", "axe_gemm_grouped_pair_static", "axe_gemm_grouped_kernel", "axe_gemm_grouped_describe", "axe_gemm_tile", "axe_gemm_describe", "axe_strerror",
            "axe_last_error", "axe_version", "axe_layout_span", "axe_layout_canonicalize", "axe_layout_gap_condition",
            "axe_layout_equal", "axe_layout_group", "axe_layout_tile", "axe_layout_direct_sum", "axe_layout_flatten", "axe_layout_tile_of",
-           "axe_layout_slice"]
+           "axe_layout_slice",
+           "axe_rmsnorm", "axe_rmsnorm_backward", "axe_rmsnorm_workspace", "axe_route", "axe_route_backward", "axe_route_workspace",
+           "axe_rows_dispatch", "axe_rows_combine", "axe_rows_combine_backward"]
 
 
 class axe_iter_t(C.Structure):
@@ -62,6 +66,25 @@ class axe_gemm_grouped_desc_t(C.Structure):
                 ("mem_axis", C.c_int32),
                 ("a_elems", C.c_int64), ("b_elems", C.c_int64), ("c_elems", C.c_int64), ("epilogue", C.c_int32),
                 ("kernel_hint", C.c_int32), ("d_scale_a", C.c_void_p), ("d_scale_b", C.c_void_p), ("scale_dtype", C.c_int32)]
+
+
+class axe_rmsnorm_desc_t(C.Structure):
+    _fields_ = [("T", C.c_int64), ("H", C.c_int64), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("weight_dtype", C.c_int32),
+                ("scale_dtype", C.c_int32), ("eps", C.c_float), ("mem_axis", C.c_int32),
+                ("x", axe_layout_t), ("residual", axe_layout_t), ("sum", axe_layout_t), ("y", axe_layout_t),
+                ("x_elems", C.c_int64), ("residual_elems", C.c_int64), ("sum_elems", C.c_int64), ("y_elems", C.c_int64)]
+
+
+class axe_route_desc_t(C.Structure):
+    _fields_ = [("T", C.c_int64), ("E", C.c_int32), ("k", C.c_int32), ("logit_dtype", C.c_int32), ("score", C.c_int32), ("renorm", C.c_int32),
+                ("groups", C.c_int32), ("groups_kept", C.c_int32), ("group_score", C.c_int32), ("scale", C.c_float), ("mem_axis", C.c_int32),
+                ("logits", axe_layout_t), ("logits_elems", C.c_int64), ("d_bias", C.c_void_p)]
+
+
+class axe_rows_desc_t(C.Structure):
+    _fields_ = [("T", C.c_int64), ("M", C.c_int64), ("H", C.c_int64), ("k", C.c_int32), ("tokens_dtype", C.c_int32), ("rows_dtype", C.c_int32),
+                ("scale_dtype", C.c_int32), ("mem_axis", C.c_int32), ("tokens", axe_layout_t), ("rows", axe_layout_t),
+                ("tokens_elems", C.c_int64), ("rows_elems", C.c_int64)]
 
 
 class AxeError(RuntimeError):
@@ -110,6 +133,15 @@ def load(path: str) -> C.CDLL:
     L.axe_gemm_describe.restype = C.c_int
     L.axe_gemm_describe.argtypes = [C.POINTER(axe_gemm_desc_t), i32, LP, C.POINTER(i64), C.POINTER(i32), vp,
                                     C.c_size_t]
+    NP, RP, WP = C.POINTER(axe_rmsnorm_desc_t), C.POINTER(axe_route_desc_t), C.POINTER(axe_rows_desc_t)
+    for name, args in (("axe_rmsnorm", [NP, vp, vp, vp, vp, vp, vp, vp]), ("axe_rmsnorm_backward", [NP, vp, vp, vp, vp, vp, vp, vp, i64, vp]),
+                       ("axe_route", [RP, vp, vp, vp, vp, vp, vp, i64, vp]), ("axe_route_backward", [RP, vp, vp, vp, vp, vp]),
+                       ("axe_rows_dispatch", [WP, vp, vp, vp, vp, vp, vp]), ("axe_rows_combine", [WP, vp, vp, vp, vp, vp, vp]),
+                       ("axe_rows_combine_backward", [WP, vp, vp, vp, vp, vp, vp, vp])):
+        getattr(L, name).restype = C.c_int
+        getattr(L, name).argtypes = args
+    L.axe_rmsnorm_workspace.restype = L.axe_route_workspace.restype = i64
+    L.axe_rmsnorm_workspace.argtypes, L.axe_route_workspace.argtypes = [NP], [RP]
     P64, P32, sz = C.POINTER(i64), C.POINTER(i32), C.c_size_t
     for name, args in (("axe_layout_span", [LP, P64]), ("axe_layout_canonicalize", [LP, LP, vp, sz]),
                        ("axe_layout_gap_condition", [LP]), ("axe_layout_equal", [LP, LP]),
@@ -380,6 +412,173 @@ def axe_gemm_grouped_describe(desc: GroupedGemmDesc, which: int) -> Tuple[dict, 
     arena = C.create_string_buffer(4096)
     _check(lib().axe_gemm_grouped_describe(C.byref(desc.c), which, C.byref(out), shape, C.byref(rank), arena, len(arena)))
     return _spec_of(out), tuple(shape[i] for i in range(rank.value))
+
+
+# ---- around the experts' products: norm, routing, rows in the experts' order
+def _matrix(layout: Optional[Layout], rows: int, cols: int, elems: Optional[int], axis: str):
+    """A matrix operand: its layout (None: contiguous, row by row) and the elements of its buffer (None: as many as the layout reaches)."""
+    if layout is None:
+        layout = Layout({"D": [(max(rows, 1), cols, axis), (cols, 1, axis)]})
+    if elems is None:
+        a = layout.axis(axis)
+        reach = sum((it.extent - 1) * it.stride for it in layout._d[:layout.c.n_d] if it.axis == a and it.stride > 0)
+        elems = layout._o[a] + reach + 1 if rows else 0
+    return layout, elems
+
+
+def _axis_of(axis: str, *layouts: Layout) -> int:
+    a = layouts[0].axis(axis)
+    assert all(L.axis(axis) == a for L in layouts), "memory axis must have the same index in all layouts"
+    return a
+
+
+def _ptr(t, elems: int = 0):
+    """The address of a device tensor that holds at least `elems` elements (None stays None)."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.numel() >= elems, "operands are device tensors of at least the elements that their layouts reach"
+    return t.data_ptr()
+
+
+def _flat(t, elems: int, dtype: str):
+    """The same of an array without a layout: contiguous, of one type."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.is_contiguous() and t.numel() >= elems and str(t.dtype) == dtype, f"{elems} contiguous elements of {dtype} on the device"
+    return t.data_ptr()
+
+
+class RmsNormDesc:
+    """Holder of an axe_rmsnorm_desc_t.  Layouts of the (T, H) matrices x, residual, sum, y default to contiguous rows, the weights' type to fp32."""
+
+    def __init__(self, T: int, H: int, x_dtype: int, y_dtype: int, eps: float = 1e-6, weight_dtype: int = AXE_F32, scale_dtype: int = AXE_SCALE_F32,
+                 x: Optional[Layout] = None, residual: Optional[Layout] = None, sum: Optional[Layout] = None, y: Optional[Layout] = None,
+                 x_elems: Optional[int] = None, residual_elems: Optional[int] = None, sum_elems: Optional[int] = None, y_elems: Optional[int] = None,
+                 mem_axis: str = "m"):
+        m = [_matrix(L, T, H, n, mem_axis) for L, n in ((x, x_elems), (residual, residual_elems), (sum, sum_elems), (y, y_elems))]
+        self.layouts = tuple(L for L, _ in m)
+        self.c = axe_rmsnorm_desc_t(T, H, x_dtype, y_dtype, weight_dtype, scale_dtype, eps, _axis_of(mem_axis, *self.layouts), *[L.c for L in self.layouts],
+                                    *[n for _, n in m])
+        self.ref = C.byref(self.c)
+        self.elems = tuple(n for _, n in m)
+        self.scale_elems = T * (-(-H // 128))
+
+
+def axe_rmsnorm(desc: RmsNormDesc, x, weight, y, residual=None, sum_out=None, scales=None, stream=None):
+    """y = norm(x + residual) * weight; sum_out receives x + residual, scales those of an e4m3 y."""
+    ex, er, es, ey = desc.elems
+    rc = (_lib or lib()).axe_rmsnorm(desc.ref, _ptr(x, ex), _ptr(residual, er), _ptr(weight, desc.c.H), _ptr(sum_out, es), _ptr(y, ey), _ptr(scales, desc.scale_elems),
+                                     _stream_ptr(stream))
+    if rc:
+        _check(rc)
+    return y
+
+
+def axe_rmsnorm_workspace(desc: RmsNormDesc) -> int:
+    """4-byte words of the workspace that axe_rmsnorm_backward with a dweight needs."""
+    return _count(lib().axe_rmsnorm_workspace(desc.ref))
+
+
+def axe_rmsnorm_backward(desc: RmsNormDesc, dy, sum, weight, dx, dsum=None, dweight=None, workspace=None, stream=None):
+    """Gradients of x (and of residual) and, with dweight, of the weights; `sum` is the normed rows, dsum what arrives at them otherwise."""
+    ex, er, es, ey = desc.elems
+    rc = (_lib or lib()).axe_rmsnorm_backward(desc.ref, _ptr(dy, ey), _ptr(sum, es), _ptr(weight, desc.c.H), _ptr(dsum, er), _ptr(dx, ex),
+                                              _flat(dweight, desc.c.H, "torch.float32"), *_words(workspace), _stream_ptr(stream))
+    if rc:
+        _check(rc)
+    return dx
+
+
+class RouteDesc:
+    """Holder of an axe_route_desc_t (keeps the bias alive).  logits: layout of (T, E), default contiguous rows."""
+
+    def __init__(self, T: int, E: int, k: int, logit_dtype: int = AXE_F32, score: int = AXE_ROUTE_SOFTMAX, renorm: bool = True, groups: int = 1,
+                 groups_kept: int = 1, group_score: int = AXE_ROUTE_GROUP_MAX, scale: float = 1.0, bias=None, logits: Optional[Layout] = None,
+                 logits_elems: Optional[int] = None, mem_axis: str = "m"):
+        L, n = _matrix(logits, T, E, logits_elems, mem_axis)
+        self.layouts, self.bias, self.elems, self.pairs = (L,), bias, n, T * k
+        self.c = axe_route_desc_t(T, E, k, logit_dtype, score, int(bool(renorm)), groups, groups_kept, group_score, scale, L.axis(mem_axis), L.c, n,
+                                  _flat(bias, E, "torch.float32"))
+        self.ref = C.byref(self.c)
+
+
+def axe_route(desc: RouteDesc, logits, ids, weights, group_rows=None, row_of=None, workspace=None, stream=None):
+    """Chosen experts (int32) and weights (fp32) of every token; group_rows (int32, E + 1) and row_of (int32, as ids): the experts' order of the pairs."""
+    rc = (_lib or lib()).axe_route(desc.ref, _ptr(logits, desc.elems), _flat(ids, desc.pairs, "torch.int32"), _flat(weights, desc.pairs, "torch.float32"),
+                                   _flat(group_rows, desc.c.E + 1, "torch.int32"), _flat(row_of, desc.pairs, "torch.int32"), *_words(workspace), _stream_ptr(stream))
+    if rc:
+        _check(rc)
+    return ids, weights
+
+
+def axe_route_workspace(desc: RouteDesc) -> int:
+    """4-byte words of the workspace that axe_route with the experts' order needs."""
+    return _count(lib().axe_route_workspace(desc.ref))
+
+
+def axe_route_backward(desc: RouteDesc, logits, ids, dweights, dlogits, stream=None):
+    """Gradient of the logits from that of the weights."""
+    rc = (_lib or lib()).axe_route_backward(desc.ref, _ptr(logits, desc.elems), _flat(ids, desc.pairs, "torch.int32"), _flat(dweights, desc.pairs, "torch.float32"),
+                                            _ptr(dlogits, desc.elems), _stream_ptr(stream))
+    if rc:
+        _check(rc)
+    return dlogits
+
+
+class RowsDesc:
+    """Holder of an axe_rows_desc_t: T tokens of k rows each, M rows in the experts' order; layouts of tokens (T, H) and rows (M, H) default to
+    contiguous rows."""
+
+    def __init__(self, T: int, k: int, M: int, H: int, tokens_dtype: int, rows_dtype: int, scale_dtype: int = AXE_SCALE_F32, tokens: Optional[Layout] = None,
+                 rows: Optional[Layout] = None, tokens_elems: Optional[int] = None, rows_elems: Optional[int] = None, mem_axis: str = "m"):
+        (Lt, nt), (Lr, nr) = _matrix(tokens, T, H, tokens_elems, mem_axis), _matrix(rows, M, H, rows_elems, mem_axis)
+        self.layouts, self.elems, self.pairs, self.nb = (Lt, Lr), (nt, nr), T * k, -(-H // 128)
+        self.c = axe_rows_desc_t(T, M, H, k, tokens_dtype, rows_dtype, scale_dtype, _axis_of(mem_axis, Lt, Lr), Lt.c, Lr.c, nt, nr)
+        self.ref = C.byref(self.c)
+
+
+def axe_rows_dispatch(desc: RowsDesc, tokens, row_of, rows, token_scales=None, scales=None, stream=None):
+    """rows[row_of[t][j]] = tokens[t], quantised where the rows are e4m3 (row_of None: the rows are in order already)."""
+    nt, nr = desc.elems
+    rc = (_lib or lib()).axe_rows_dispatch(desc.ref, _ptr(tokens, nt), _ptr(token_scales, desc.c.T * desc.nb), _flat(row_of, desc.pairs, "torch.int32"), _ptr(rows, nr),
+                                           _ptr(scales, desc.c.M * desc.nb), _stream_ptr(stream))
+    if rc:
+        _check(rc)
+    return rows
+
+
+def axe_rows_combine(desc: RowsDesc, rows, row_of, weights, tokens, add=None, stream=None):
+    """tokens[t] = add[t] + sum_j weights[t][j] rows[row_of[t][j]] (weights None: ones)."""
+    nt, nr = desc.elems
+    rc = (_lib or lib()).axe_rows_combine(desc.ref, _ptr(rows, nr), _flat(row_of, desc.pairs, "torch.int32"), _flat(weights, desc.pairs, "torch.float32"), _ptr(add, nt),
+                                          _ptr(tokens, nt), _stream_ptr(stream))
+    if rc:
+        _check(rc)
+    return tokens
+
+
+def axe_rows_combine_backward(desc: RowsDesc, dtokens, rows, row_of, weights, drows=None, dweights=None, stream=None):
+    """Gradients of the rows and of the weights from that of the tokens."""
+    nt, nr = desc.elems
+    rc = (_lib or lib()).axe_rows_combine_backward(desc.ref, _ptr(dtokens, nt), _ptr(rows, nr), _flat(row_of, desc.pairs, "torch.int32"),
+                                                   _flat(weights, desc.pairs, "torch.float32"), _ptr(drows, nr), _flat(dweights, desc.pairs, "torch.float32"),
+                                                   _stream_ptr(stream))
+    if rc:
+        _check(rc)
+    return drows, dweights
+
+
+def _words(workspace):
+    if workspace is None:
+        return None, 0
+    assert workspace.is_cuda and workspace.is_contiguous() and workspace.itemsize == 4
+    return workspace.data_ptr(), workspace.numel()
+
+
+def _count(n: int) -> int:
+    if n < 0:
+        _check(n)
+    return n
 
 
 # ---- layout operators (host only; the library does the work, this only marshals)

@@ -9,16 +9,65 @@
 #include "../../include/axe.h"
 #include "host_layout.h"
 #include "kernels.h"
+#include "plans.h"
 #include "tile_family.h"
 
 using namespace axe;
 
-namespace {
-
-int hip_fail(hipError_t e, const char* what) {
+int axe::hip_fail(hipError_t e, const char* what) {
   set_error("%s: HIP error %d (%s)", what, (int)e, hipGetErrorString(e));
   return AXE_EHIP;
 }
+
+// A 2-D operand whose canonical memory layout is "unit stride along `inner`, pitch along
+// `outer`": returns pitch and offset.  `outer_first` tells which logical dim comes first.
+int axe::strided_2d(const axe_layout_t* L, int mem_axis, int64_t d0, int64_t d1, bool inner_is_dim1, int64_t elems,
+               const char* what, int64_t* pitch, int64_t* offset) {
+  HLayout h;
+  if (int rc = load_layout(L, h, what)) return rc;
+  int64_t shape[2] = {d0, d1};
+  if (int rc = check_shape(h, 2, shape, what)) return rc;
+  MemLayout m;
+  if (int rc = reduce_to_memory(h, mem_axis, m, what)) return rc;
+  if (!m.R.empty()) {
+    set_error("%s: replicated operands are not supported", what);
+    return AXE_EUNSUPPORTED;
+  }
+  if (m.swz.mask) {
+    set_error("%s: swizzled operands are not supported", what);
+    return AXE_EUNSUPPORTED;
+  }
+  if (int rc = check_range(m, elems, what)) return rc;
+  const int64_t inner = inner_is_dim1 ? d1 : d0, outer = inner_is_dim1 ? d0 : d1;
+  // canonical forms accepted: [(outer, pitch), (inner, 1)] in logical order (or swapped when the
+  // inner dim is logical dim 0), or a single merged iter (outer*inner, 1) when pitch == inner
+  std::vector<HIter>& D = m.D;
+  int64_t p = 0;
+  bool ok = false;
+  if (D.empty()) {
+    ok = (d0 == 1 && d1 == 1);
+    p = inner;
+  } else if (D.size() == 1) {
+    if (D[0].s == 1 && D[0].e == d0 * d1 && (outer == 1 || inner_is_dim1)) ok = true, p = inner;      // contiguous
+    else if (inner == 1 && D[0].e == outer) ok = true, p = D[0].s;
+    else if (outer == 1 && D[0].e == inner && D[0].s == 1) ok = true, p = inner;
+  } else if (D.size() == 2) {
+    const HIter& a = D[0];
+    const HIter& b = D[1];
+    if (inner_is_dim1 && a.e == d0 && b.e == d1 && b.s == 1) ok = true, p = a.s;
+    if (!inner_is_dim1 && a.e == d0 && b.e == d1 && a.s == 1) ok = true, p = b.s;
+  }
+  if (!ok || p < inner) {
+    set_error("%s: layout is not a pitched matrix with unit stride along the %s dimension", what,
+              inner_is_dim1 ? "second" : "first");
+    return AXE_EUNSUPPORTED;
+  }
+  *pitch = p;
+  *offset = m.off;
+  return AXE_OK;
+}
+
+namespace {
 
 int ilog2(int64_t v) {
   int l = 0;
@@ -32,45 +81,12 @@ int env_int(const char* name, int dflt) {
   return s && *s ? atoi(s) : dflt;
 }
 
-// The contents of a descriptor as a flat run of words: what a plan depends on, device pointers aside (of those
-// only whether they are given and their alignment matter).  False when the descriptor is malformed in a way
-// that makes its arrays unreadable: the planner then reports the error.
-constexpr int kKeyWords = 24 + 3 * (12 + 3 * (AXE_MAX_D + AXE_MAX_R) + AXE_MAX_AXES);
-struct PlanKey {
-  int64_t w[kKeyWords];
-  int n = 0;
-  void put(int64_t v) { w[n++] = v; }
-};
-bool key_of_layout(const axe_layout_t& L, PlanKey& k) {
-  if (L.n_axes < 1 || L.n_axes > AXE_MAX_AXES || L.n_d < 1 || L.n_d > AXE_MAX_D || L.n_r < 0 || L.n_r > AXE_MAX_R || !L.d ||
-      (L.n_r && !L.r))
-    return false;
-  k.put(L.n_axes), k.put(L.n_d), k.put(L.n_r);
-  for (int i = 0; i < L.n_d; ++i) k.put(L.d[i].extent), k.put(L.d[i].stride), k.put(L.d[i].axis);
-  for (int i = 0; i < L.n_r; ++i) k.put(L.r[i].extent), k.put(L.r[i].stride), k.put(L.r[i].axis);
-  for (int a = 0; a < L.n_axes; ++a) k.put(L.offset ? L.offset[a] : 0);
-  k.put(L.swz_axis), k.put(L.swz_bits), k.put(L.swz_base), k.put(L.swz_shift);
-  return true;
-}
-
 // Whether any of the library's knobs is set (they are read whenever a call is planned: no plan is kept then).
 bool knobs_set() {
   for (char** e = environ; e && *e; ++e)
     if ((*e)[0] == 'A' && (*e)[1] == 'X' && (*e)[2] == 'E' && (*e)[3] == '_') return true;
   return false;
 }
-
-// The plan of the last call of one kind that this thread made: a caller that moves or evaluates the same layouts again
-// (compared word by word; other buffers of the same alignment are fine) skips the layout analysis, 1 - 1.5 us of a
-// call whose launch takes 2.5.
-template <class Plan>
-struct LastPlan {
-  PlanKey key;
-  Plan plan;
-  bool have = false;
-  bool holds(const PlanKey& k) const { return have && k.n == key.n && memcmp(k.w, key.w, sizeof(int64_t) * k.n) == 0; }
-  void keep(const PlanKey& k, const Plan& p) { key = k, plan = p, have = true; }
-};
 
 // A planned relayout: which kernel, and its plan.
 struct RelayoutCall {
@@ -627,55 +643,6 @@ bool key_of_gemm(const axe_gemm_desc_t* g, PlanKey& k) {
   k.put((int64_t)(((uintptr_t)g->d_scale_a | (uintptr_t)g->d_scale_b) & 3));
   return key_of_layout(g->A, k) && key_of_layout(g->B, k) && key_of_layout(g->C, k);
 }
-
-// A 2-D operand whose canonical memory layout is "unit stride along `inner`, pitch along
-// `outer`": returns pitch and offset.  `outer_first` tells which logical dim comes first.
-int strided_2d(const axe_layout_t* L, int mem_axis, int64_t d0, int64_t d1, bool inner_is_dim1, int64_t elems,
-               const char* what, int64_t* pitch, int64_t* offset) {
-  HLayout h;
-  if (int rc = load_layout(L, h, what)) return rc;
-  int64_t shape[2] = {d0, d1};
-  if (int rc = check_shape(h, 2, shape, what)) return rc;
-  MemLayout m;
-  if (int rc = reduce_to_memory(h, mem_axis, m, what)) return rc;
-  if (!m.R.empty()) {
-    set_error("%s: replicated GEMM operands are not supported", what);
-    return AXE_EUNSUPPORTED;
-  }
-  if (m.swz.mask) {
-    set_error("%s: swizzled HBM operands are not supported by axe_gemm", what);
-    return AXE_EUNSUPPORTED;
-  }
-  if (int rc = check_range(m, elems, what)) return rc;
-  const int64_t inner = inner_is_dim1 ? d1 : d0, outer = inner_is_dim1 ? d0 : d1;
-  // canonical forms accepted: [(outer, pitch), (inner, 1)] in logical order (or swapped when the
-  // inner dim is logical dim 0), or a single merged iter (outer*inner, 1) when pitch == inner
-  std::vector<HIter>& D = m.D;
-  int64_t p = 0;
-  bool ok = false;
-  if (D.empty()) {
-    ok = (d0 == 1 && d1 == 1);
-    p = inner;
-  } else if (D.size() == 1) {
-    if (D[0].s == 1 && D[0].e == d0 * d1 && (outer == 1 || inner_is_dim1)) ok = true, p = inner;      // contiguous
-    else if (inner == 1 && D[0].e == outer) ok = true, p = D[0].s;
-    else if (outer == 1 && D[0].e == inner && D[0].s == 1) ok = true, p = inner;
-  } else if (D.size() == 2) {
-    const HIter& a = D[0];
-    const HIter& b = D[1];
-    if (inner_is_dim1 && a.e == d0 && b.e == d1 && b.s == 1) ok = true, p = a.s;
-    if (!inner_is_dim1 && a.e == d0 && b.e == d1 && a.s == 1) ok = true, p = b.s;
-  }
-  if (!ok || p < inner) {
-    set_error("%s: layout is not a pitched matrix with unit stride along the %s dimension", what,
-              inner_is_dim1 ? "second" : "first");
-    return AXE_EUNSUPPORTED;
-  }
-  *pitch = p;
-  *offset = m.off;
-  return AXE_OK;
-}
-
 
 // An input operand that is not a plain pitched matrix may still be a blocked one (Sec. 3.3: a tile product
 // of a grid of blocks and a block): grouped by its logical shape (Alg. 1), the k block is

@@ -9,6 +9,7 @@
 
 #include "device_types.h"
 #include "kernels.h"
+#include "layer_ops.h"
 #include "tile_family.h"
 
 namespace axe {
@@ -338,6 +339,15 @@ hipError_t launch_gemm_grouped_stream(const GemmArgs& g, hipStream_t) { return g
 hipError_t launch_gemm_fp8_256(const GemmArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_gemm_fp8_e8m0_256(const GemmArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_gemm_fp8_e8m0_256_grouped(const GemmArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rmsnorm(const NormArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rmsnorm_backward(const NormArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_route(const RouteArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_route_backward(const RouteArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rows_dispatch(const RowsArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rows_combine(const RowsArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rows_combine_backward(const RowsArgs&, hipStream_t) { return hipErrorNotSupported; }
+int64_t rmsnorm_workspace_words(int64_t, int64_t) { return 0; }
+int64_t route_workspace_words(int64_t, int, int) { return 0; }
 
 }  // namespace axe
 
