@@ -8,44 +8,184 @@
 
 namespace axe {
 
-template <int TYPE>
-struct ElemOf;
-template <>
-struct ElemOf<kBf16> { using T = __bf16; };
-template <>
-struct ElemOf<kF16> { using T = _Float16; };
-template <>
-struct ElemOf<kF32> { using T = float; };
-template <>
-struct ElemOf<kFp8> { using T = uint8_t; };
-
+// One element, of a type known at run time only.
 __device__ __forceinline__ float load_elem(const void* p, int64_t i, int type) {
   return type == kBf16 ? (float)((const __bf16*)p)[i] : type == kF16 ? (float)((const _Float16*)p)[i] : ((const float*)p)[i];
 }
-__device__ __forceinline__ void store_elem(void* p, int64_t i, int type, float v) {
-  if (type == kBf16) ((__bf16*)p)[i] = (__bf16)v;
-  else if (type == kF16) ((_Float16*)p)[i] = (_Float16)v;
-  else ((float*)p)[i] = v;
+
+// Eight neighbouring elements of a row, as bits: 16 bytes in 16-bit types, 32 in fp32, 8 in e4m3.  The kernels give every thread such runs.  They may start at any
+// element: the hardware takes 16-byte accesses at any address, so rows of odd pitches need no path of their own, they only touch more lines.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <class V>
+struct __attribute__((packed, aligned(1))) Anywhere {
+  V v;
+};
+template <class V>
+__device__ __forceinline__ V load_bits(const void* p) { return ((const Anywhere<V>*)p)->v; }
+template <class V>
+__device__ __forceinline__ void store_bits(void* p, V v) { ((Anywhere<V>*)p)->v = v; }
+
+template <int TYPE>
+struct Run8;
+template <>
+struct Run8<kBf16> {
+  using Elem = uint16_t;
+  u32x4 b;
+  __device__ __forceinline__ void clear() { b = u32x4{}; }
+  __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x4>(p); }
+  __device__ __forceinline__ void store(void* p) const { store_bits(p, b); }
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? b[i >> 1] & 0xffff0000u : b[i >> 1] << 16); }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+      b[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});    // round to nearest even
+    }
+  }
+  __device__ __forceinline__ Elem elem(int i) const { return (Elem)(b[i >> 1] >> (i & 1) * 16); }
+  __device__ __forceinline__ void put(int i, Elem e) { b[i >> 1] = i & 1 ? (b[i >> 1] & 0xffffu) | (uint32_t)e << 16 : (b[i >> 1] & 0xffff0000u) | e; }
+};
+template <>
+struct Run8<kF16> {
+  using Elem = uint16_t;
+  u32x4 b;
+  __device__ __forceinline__ void clear() { b = u32x4{}; }
+  __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x4>(p); }
+  __device__ __forceinline__ void store(void* p) const { store_bits(p, b); }
+  __device__ __forceinline__ float get(int i) const { return (float)__builtin_bit_cast(_Float16, (uint16_t)(b[i >> 1] >> (i & 1) * 16)); }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+      b[i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)v[2 * i], (_Float16)v[2 * i + 1]});
+    }
+  }
+  __device__ __forceinline__ Elem elem(int i) const { return (Elem)(b[i >> 1] >> (i & 1) * 16); }
+  __device__ __forceinline__ void put(int i, Elem e) { b[i >> 1] = i & 1 ? (b[i >> 1] & 0xffffu) | (uint32_t)e << 16 : (b[i >> 1] & 0xffff0000u) | e; }
+};
+template <>
+struct Run8<kF32> {
+  using Elem = uint32_t;
+  u32x4 b[2];
+  __device__ __forceinline__ void clear() { b[0] = b[1] = u32x4{}; }
+  __device__ __forceinline__ void load(const void* p) { b[0] = load_bits<u32x4>(p), b[1] = load_bits<u32x4>((const char*)p + 16); }
+  __device__ __forceinline__ void store(void* p) const { store_bits(p, b[0]), store_bits((char*)p + 16, b[1]); }
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(b[i >> 2][i & 3]); }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i >> 2][i & 3] = __float_as_uint(v[i]);
+  }
+  __device__ __forceinline__ Elem elem(int i) const { return b[i >> 2][i & 3]; }
+  __device__ __forceinline__ void put(int i, Elem e) { b[i >> 2][i & 3] = e; }
+};
+template <>
+struct Run8<kFp8> {
+  using Elem = uint8_t;
+  u32x2 b;
+  __device__ __forceinline__ void clear() { b = u32x2{}; }
+  __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x2>(p); }
+  __device__ __forceinline__ void store(void* p) const { store_bits(p, b); }
+  __device__ __forceinline__ void set(const float (&v)[8]);
+  __device__ __forceinline__ Elem elem(int i) const { return (Elem)(b[i >> 2] >> (i & 3) * 8); }
+  __device__ __forceinline__ void put(int i, Elem e) { b[i >> 2] = (b[i >> 2] & ~(0xffu << (i & 3) * 8)) | (uint32_t)e << (i & 3) * 8; }
+};
+
+// The run at element i of a row, `left` elements before its end (none: zeros, nothing read).
+template <int TYPE>
+__device__ __forceinline__ void load_run(Run8<TYPE>& r, const void* row, int64_t i, int left) {
+  using E = typename Run8<TYPE>::Elem;
+  const E* p = (const E*)row + i;
+  if (left >= 8) {
+    r.load(p);
+    return;
+  }
+  r.clear();
+#pragma unroll
+  for (int k = 0; k < 7; ++k)
+    if (k < left) r.put(k, p[k]);
+}
+template <int TYPE>
+__device__ __forceinline__ void store_run(const Run8<TYPE>& r, void* row, int64_t i, int left) {
+  using E = typename Run8<TYPE>::Elem;
+  E* p = (E*)row + i;
+  if (left >= 8) {
+    r.store(p);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 7; ++k)
+    if (k < left) p[k] = r.elem(k);
+}
+// Weights of a type known at run time, as fp32; null: ones.
+__device__ __forceinline__ void load_weights(float (&w)[8], const void* p, int type, int64_t i, int left) {
+  if (!p) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+  } else if (type == kF32) {
+    Run8<kF32> r;
+    load_run(r, p, i, left);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = r.get(k);
+  } else if (type == kBf16) {
+    Run8<kBf16> r;
+    load_run(r, p, i, left);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = r.get(k);
+  } else {
+    Run8<kF16> r;
+    load_run(r, p, i, left);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = r.get(k);
+  }
 }
 
-// The sum over a wave, in every lane.
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+// Exchanges inside a row of 16 lanes are operands of the instruction that uses them (DPP); between rows gfx950 swaps whole rows.
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false); }
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+struct Add {
+  __device__ __forceinline__ static float of(float a, float b) { return a + b; }
+};
+struct Max {
+  __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); }
+};
+// v of all 16 lanes of a row, or of all 64, joined, in every lane.  (Each step joins lanes that hold the same number of values: the
+// two sides of a step are the same in both lanes, so the results are the same bits.)
+template <class OP>
+__device__ __forceinline__ float row16_all(float v) {
+  v = OP::of(v, __int_as_float(dpp<kXor1>(__float_as_int(v))));
+  v = OP::of(v, __int_as_float(dpp<kXor2>(__float_as_int(v))));
+  v = OP::of(v, __int_as_float(dpp<kHalfMirror>(__float_as_int(v))));
+  return OP::of(v, __int_as_float(dpp<kMirror>(__float_as_int(v))));
 }
-// The sum over a workgroup of WAVES waves, in every thread; lds: WAVES floats, free again after the caller's next barrier.
-template <int WAVES>
-__device__ __forceinline__ float group_sum(float v, float* lds) {
-  v = wave_sum(v);
-  if (WAVES == 1) return v;
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float t = 0;
+template <class OP>
+__device__ __forceinline__ float wave_all(float v) {
+  v = row16_all<OP>(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+  v = OP::of(__int_as_float(a[0]), __int_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+  return OP::of(__int_as_float(b[0]), __int_as_float(b[1]));
+}
+__device__ __forceinline__ float wave_sum(float v) { return wave_all<Add>(v); }
+// The sums of N values over the threads of a row that WAVES waves hold, in every thread.  lds: N x WAVES floats of the row; what was read from it before a
+// barrier may be overwritten.
+template <int N, int WAVES>
+__device__ __forceinline__ void row_sums(float (&v)[N], float* lds) {
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) t += lds[i];
+  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+  if (WAVES == 1) return;
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) lds[i * WAVES + (threadIdx.x >> 6)] = v[i];
   __syncthreads();
-  return t;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float t = 0;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) t += lds[i * WAVES + k];
+    v[i] = t;
+  }
 }
 
 // The scale of 128 columns whose largest magnitude is `most` (NaNs left out): s, and 1 / s, which the columns are multiplied by.  fp32: most / 448, not below
@@ -78,6 +218,12 @@ __device__ __forceinline__ float clamp_e4m3(float v) { return fabsf(v) > 448.0f 
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(a), clamp_e4m3(b), 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(c), clamp_e4m3(d), w, true);
+}
+
+__device__ __forceinline__ void Run8<kFp8>::set(const float (&v)[8]) { b = u32x2{pack_e4m3(v[0], v[1], v[2], v[3]), pack_e4m3(v[4], v[5], v[6], v[7])}; }
+__device__ __forceinline__ void store_scale(void* scales, int64_t i, const Scale& s, bool e8m0) {
+  if (e8m0) ((uint8_t*)scales)[i] = (uint8_t)s.code;
+  else ((float*)scales)[i] = s.s;
 }
 
 }  // namespace axe
