@@ -417,7 +417,7 @@ int64_t axe_route_workspace(const axe_route_desc_t* g);       /* words, or a neg
  *   (ones); d_add (layout and type of tokens) or NULL, may be d_tokens.  A weight of 0 does not make a row absent (0 * inf is NaN); an entry that is no row does.
  * axe_rows_combine_backward -- d_drows[row_of[t][j]] = weights[t][j] dtokens[t] (layout and type of rows; may be d_rows) and
  *   d_dweights[t][j] = sum_c dtokens[t][c] rows[row_of[t][j]][c] (0 where there is no row).  Either output may be NULL; d_rows may be NULL without d_dweights.
- * The last two: one type, AXE_BF16, AXE_F16 or AXE_F32.  k up to 64; H, M below 2^31. */
+ * The last two: one type, AXE_BF16, AXE_F16 or AXE_F32.  k up to 64; M and T k below 2^31, H below 2^28. */
 typedef struct {
   int64_t      T, M, H;
   int32_t      k;

@@ -171,8 +171,8 @@ int check_rows(const axe_rows_desc_t* g, const char* fn, bool dispatch) {
   if (g->scale_dtype != AXE_SCALE_F32 && g->scale_dtype != AXE_SCALE_E8M0) return invalid(fn, "unknown scale_dtype");
   if (g->tokens_dtype != g->rows_dtype && !(dispatch && g->rows_dtype == AXE_FP8_E4M3)) return unsupported(fn, "tokens and rows have one type (dispatch: or the rows are e4m3)");
   if (!dispatch && g->rows_dtype == AXE_FP8_E4M3) return unsupported(fn, "rows in 16 or 32 bits");
-  if (g->k > kRowsMaxK || g->H >= (int64_t(1) << 31) || g->M >= (int64_t(1) << 31) || g->T >= (int64_t(1) << 31) / g->k)
-    return unsupported(fn, "k up to 64; H, M and T k below 2^31");
+  if (g->k > kRowsMaxK || g->H >= (int64_t(1) << 28) || g->M >= (int64_t(1) << 31) || g->T >= (int64_t(1) << 31) / g->k)
+    return unsupported(fn, "k up to 64; M and T k below 2^31, H below 2^28");
   return AXE_OK;
 }
 int kept_rows_plan(const axe_rows_desc_t* g, const char* fn, RowsPlan& out) {

@@ -10,51 +10,56 @@
 
 namespace axe {
 
-// Threads of a workgroup whose rows have TPR threads each: rows of one wave go four to a workgroup.
-constexpr int norm_threads(int tpr) { return tpr < 256 ? 256 : tpr; }
-
-// XT: x, residual and sum; YT: y.  A row of up to TPR * 8 * RUNS columns.
-template <int XT, int YT, int TPR, int RUNS>
-__global__ __launch_bounds__(norm_threads(TPR)) void rmsnorm_kernel(NormArgs a) {
-  constexpr int WAVES = TPR / 64;
+// XT: x, residual and sum; YT: y.  A row of up to TPR * 8 * RUNS columns; SHORT: of fewer than 8.
+template <int XT, int YT, int TPR, int RUNS, bool SHORT>
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_kernel(NormArgs a) {
+  constexpr int WAVES = TPR / 64, ROWS = TPR == 64 ? 4 : 1;
   __shared__ float lds[WAVES];
-  const int tid = threadIdx.x % TPR;
-  const int64_t t = (int64_t)blockIdx.x * (norm_threads(TPR) / TPR) + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+  const int c = threadIdx.x % TPR * 8;                             // column of the thread's first run
+  const int64_t t = (int64_t)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
   if (t >= a.T) return;                                            // (whole waves of rows of one wave, or none)
   Run8<XT> x[RUNS], r[RUNS];
-  float w[RUNS][8];
+  const void *rx = elem_at(a.x, t * a.ldx, elem_bytes(XT)), *rr = elem_at(a.r, t * a.ldr, elem_bytes(XT));
 #pragma unroll
-  for (int i = 0; i < RUNS; ++i) {
-    const int c = (i * TPR + tid) * 8, left = a.H - c;
-    load_run(x[i], a.x, t * a.ldx + c, left);
-    if (a.r) load_run(r[i], a.r, t * a.ldr + c, left);
+  for (int i = 0; i < RUNS; ++i) load_run<SHORT>(x[i], rx, c + i * TPR * 8, a.H);
+  if (a.r) {
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i) load_run<SHORT>(r[i], rr, c + i * TPR * 8, a.H);
+  } else {
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i) r[i].clear();
   }
-#pragma unroll
-  for (int i = 0; i < RUNS; ++i) load_weights(w[i], a.w, a.w_type, (i * TPR + tid) * 8, a.H - (i * TPR + tid) * 8);
+  float w[RUNS][8];
+  load_weights<SHORT, TPR>(w, a.w, a.w_type, c, a.H);
   float h[RUNS][8], sq[1] = {0};
 #pragma unroll
-  for (int i = 0; i < RUNS; ++i)
+  for (int i = 0; i < RUNS; ++i) {
+    end_run<SHORT>(x[i], c + i * TPR * 8, a.H);
+    end_run<SHORT>(r[i], c + i * TPR * 8, a.H);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      h[i][k] = a.r ? x[i].get(k) + r[i].get(k) : x[i].get(k);
+      h[i][k] = x[i].get(k) + r[i].get(k);
       sq[0] += h[i][k] * h[i][k];
     }
+  }
   if (a.sum) {
+    void* rs = elem_at(a.sum, t * a.lds, elem_bytes(XT));
 #pragma unroll
     for (int i = 0; i < RUNS; ++i) {
-      const int c = (i * TPR + tid) * 8;
       x[i].set(h[i]);
-      store_run(x[i], a.sum, t * a.lds + c, a.H - c);
+      store_run(x[i], rs, c + i * TPR * 8, a.H);
     }
   }
-  row_sums<1, WAVES>(sq, lds);
+  row_sums<1, WAVES>(sq, lds, threadIdx.x % TPR >> 6);
   const float rho = 1.0f / sqrtf(sq[0] / (float)a.H + a.eps);
+  void* ry = elem_at(a.y, t * a.ldy, elem_bytes(YT));
 #pragma unroll
   for (int i = 0; i < RUNS; ++i) {
-    const int c = (i * TPR + tid) * 8, left = a.H - c;
+    const int ci = c + i * TPR * 8;
     float y[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) y[k] = h[i][k] * rho * w[i][k];
+    Run8<YT> q;
     if constexpr (YT == kFp8) {
       float most = 0;
 #pragma unroll
@@ -62,66 +67,70 @@ __global__ __launch_bounds__(norm_threads(TPR)) void rmsnorm_kernel(NormArgs a) 
       const Scale s = scale_of(row16_all<Max>(most), a.e8m0);
 #pragma unroll
       for (int k = 0; k < 8; ++k) y[k] *= s.inv;
-      Run8<kFp8> q;
-      q.set(y);
-      store_run(q, a.y, t * a.ldy + c, left);
-      if ((tid & 15) == 0 && left > 0) store_scale(a.scales, t * ((a.H + 127) >> 7) + (c >> 7), s, a.e8m0);
-    } else {
-      Run8<YT> q;
-      q.set(y);
-      store_run(q, a.y, t * a.ldy + c, left);
+      if ((threadIdx.x & 15) == 0 && ci < a.H) store_scale(a.scales, t * ((a.H + 127) >> 7) + (ci >> 7), s, a.e8m0);
     }
+    q.set(y);
+    store_run(q, ry, ci, a.H);
   }
 }
 
 // Gradients.  XT: h, dsum and dx; YT: dy.  A workgroup takes every gridDim-th row (rows of one wave: four at a time) and keeps its threads' columns of dw in
 // registers; what a workgroup has of dw goes to its row of the workspace, and a second kernel adds these rows up.
-template <int XT, int YT, int TPR, int RUNS>
-__global__ __launch_bounds__(norm_threads(TPR)) void rmsnorm_backward_kernel(NormArgs a) {
-  constexpr int WAVES = TPR / 64, ROWS = norm_threads(TPR) / TPR;
-  __shared__ float lds[2][2 * WAVES];
+template <int XT, int YT, int TPR, int RUNS, int ROWS, bool SHORT>
+__global__ __launch_bounds__(TPR * ROWS) void rmsnorm_backward_kernel(NormArgs a) {
+  constexpr int WAVES = TPR / 64;
+  __shared__ float lds[2][ROWS][2 * WAVES];
   extern __shared__ float part[];
-  const int tid = threadIdx.x % TPR, sub = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+  const int tid = threadIdx.x % TPR, c = tid * 8, sub = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
   float dw[RUNS][8] = {};
   int turn = 0;
-  for (int64_t t = (int64_t)blockIdx.x * ROWS + sub; t < a.T; t += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+  for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < a.T; t0 += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+    const bool there = t0 + sub < a.T;
+    const int64_t t = there ? t0 + sub : a.T - 1;                  // (all rows of a workgroup take part in its barriers)
     Run8<YT> dy[RUNS];
     Run8<XT> h[RUNS], ds[RUNS];
+    const void *rd = elem_at(a.x, t * a.ldx, elem_bytes(YT)), *rh = elem_at(a.h, t * a.lds, elem_bytes(XT)), *rs = elem_at(a.r, t * a.ldr, elem_bytes(XT));
 #pragma unroll
     for (int i = 0; i < RUNS; ++i) {
-      const int c = (i * TPR + tid) * 8, left = a.H - c;
-      load_run(dy[i], a.x, t * a.ldx + c, left);
-      load_run(h[i], a.h, t * a.lds + c, left);
-      if (a.r) load_run(ds[i], a.r, t * a.ldr + c, left);
+      load_run<SHORT>(dy[i], rd, c + i * TPR * 8, a.H);
+      load_run<SHORT>(h[i], rh, c + i * TPR * 8, a.H);
     }
-    float s[2] = {0, 0};
-    float u[RUNS][8];
+    if (a.r) {
+#pragma unroll
+      for (int i = 0; i < RUNS; ++i) load_run<SHORT>(ds[i], rs, c + i * TPR * 8, a.H);
+    } else {
+#pragma unroll
+      for (int i = 0; i < RUNS; ++i) ds[i].clear();
+    }
+    float u[RUNS][8], s[2] = {0, 0};
+    load_weights<SHORT, TPR>(u, a.w, a.w_type, c, a.H);
 #pragma unroll
     for (int i = 0; i < RUNS; ++i) {
-      const int c = (i * TPR + tid) * 8;
-      load_weights(u[i], a.w, a.w_type, c, a.H - c);
+      end_run<SHORT>(dy[i], c + i * TPR * 8, a.H);
+      if (!there) dy[i].clear();
+      end_run<SHORT>(h[i], c + i * TPR * 8, a.H);
+      end_run<SHORT>(ds[i], c + i * TPR * 8, a.H);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         u[i][k] *= dy[i].get(k);
         s[0] += h[i].get(k) * h[i].get(k), s[1] += u[i][k] * h[i].get(k);
       }
     }
-    row_sums<2, WAVES>(s, lds[turn]);                              // (two arrays: no thread is two rows ahead of another)
+    row_sums<2, WAVES>(s, lds[turn][sub], tid >> 6);                            // (two arrays: no thread is two rows ahead of another)
     const float rho = 1.0f / sqrtf(s[0] / (float)a.H + a.eps);
     const float along = s[1] / (float)a.H * rho * rho;
+    void* ro = elem_at(a.y, t * a.ldy, elem_bytes(XT));
 #pragma unroll
     for (int i = 0; i < RUNS; ++i) {
-      const int c = (i * TPR + tid) * 8;
       float v[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        v[k] = rho * (u[i][k] - h[i].get(k) * along);
-        if (a.r) v[k] += ds[i].get(k);
+        v[k] = rho * (u[i][k] - h[i].get(k) * along) + ds[i].get(k);
         dw[i][k] += dy[i].get(k) * (h[i].get(k) * rho);
       }
       Run8<XT> out;
       out.set(v);
-      store_run(out, a.y, t * a.ldy + c, a.H - c);
+      if (there) store_run(out, ro, c + i * TPR * 8, a.H);
     }
   }
   if (!a.dw) return;
@@ -143,61 +152,75 @@ __global__ __launch_bounds__(norm_threads(TPR)) void rmsnorm_backward_kernel(Nor
   float* to = gridDim.x > 1 ? a.ws + (int64_t)blockIdx.x * a.H : a.dw;
 #pragma unroll
   for (int i = 0; i < RUNS; ++i) {
-    const int c = (i * TPR + tid) * 8;
     Run8<kF32> out;
     out.set(dw[i]);
-    store_run(out, to, c, a.H - c);
+    store_run(out, to, c + i * TPR * 8, a.H);
   }
 }
 
-// dw: the sum of n rows of the workspace.  A wave adds 16 lanes x 4 columns of four rows at a time, a workgroup 64 rows; what its waves have is joined in LDS.
+// dw: the sum of n rows of the workspace, 64 columns a workgroup: wave i adds the rows i, i + 16, ... -- loads without an order, eight in flight -- and the sums of the
+// sixteen waves are joined through LDS.
 __global__ __launch_bounds__(1024) void rmsnorm_dweight_kernel(const float* ws, float* dw, int n, int H) {
-  __shared__ float lds[64][65];
-  const int lane = threadIdx.x & 15, row = threadIdx.x >> 4, c = blockIdx.x * 64 + lane * 4;
-  float v[4] = {};
-#pragma unroll 4
-  for (int r = row; r < n; r += 64) {
-    const float* p = ws + (int64_t)r * H + c;
+  __shared__ float lds[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, at = c < H ? c : H - 1;
+  float v[8] = {};
+  int r = wave;
+  for (; r + 7 * 16 < n; r += 8 * 16)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] += c + k < H ? p[k] : 0.0f;
-  }
+    for (int k = 0; k < 8; ++k) v[k] += ws[(int64_t)(r + 16 * k) * H + at];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) lds[lane * 4 + k][row] = v[k];
+  for (int k = 0; k < 7; ++k)
+    if (r + 16 * k < n) v[k] += ws[(int64_t)(r + 16 * k) * H + at];
+  lds[wave][lane] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   __syncthreads();
-  // column threadIdx.x / 16: its 64 numbers on 16 lanes
-  const int col = threadIdx.x >> 4;
+  if (wave) return;
   float s = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) s += lds[col][lane + 16 * k];
-  s = row16_all<Add>(s);
-  if (lane == 0 && blockIdx.x * 64 + col < H) dw[blockIdx.x * 64 + col] = s;
+  for (int k = 0; k < 16; ++k) s += lds[k][lane];
+  if (c < H) dw[c] = s;
 }
 __global__ __launch_bounds__(256) void rmsnorm_no_rows_kernel(float* dw, int H) {
   if (blockIdx.x * 256 + threadIdx.x < (uint32_t)H) dw[blockIdx.x * 256 + threadIdx.x] = 0;
 }
 
-// Threads and runs of a row.
-template <int TPR_, int RUNS_>
+// Threads and runs of a row: as many threads as a run each needs, up to 512, then two and four runs.  Measured, us: 1000 x 8192 bf16 to e4m3 with 256 x 4 / 512 x 2 / 1024 x 1
+// 13.2 / 11.9 / 12.7, one row of 2048 with 64 x 4 / 256 x 1 3.4 / 2.3, fp16 2000 x 1999 6.0 / 5.8.  Backward, rows of a workgroup (of 512 or 1024 threads): it has
+// one row of the workspace to write for all of them; 4096 x 2048 bf16, 512 workgroups of 1 / 2 / 4 rows 16.1 / 14.6 / 13.6, 256 of 4 15.0, 1024 of 1 14.8.
+template <int TPR_, int RUNS_, bool SHORT_ = false>
 struct RowShape {
-  static constexpr int TPR = TPR_, RUNS = RUNS_, ROWS = norm_threads(TPR) / TPR;
+  static constexpr int TPR = TPR_, RUNS = RUNS_, ROWS = TPR == 64 ? 8 : 1024 / TPR;
+  static constexpr bool SHORT = SHORT_;
 };
 template <class F>
 void by_row_shape(int H, F&& f) {
-  if (H <= 64 * 8) f(RowShape<64, 1>());
-  else if (H <= 128 * 8) f(RowShape<64, 2>());
+  if (H < 8) f(RowShape<64, 1, true>());
+  else if (H <= 64 * 8) f(RowShape<64, 1>());
+  else if (H <= 128 * 8) f(RowShape<128, 1>());
   else if (H <= 256 * 8) f(RowShape<256, 1>());
-  else if (H <= 512 * 8) f(RowShape<256, 2>());
-  else if (H <= 1024 * 8) f(RowShape<256, 4>());
+  else if (H <= 512 * 8) f(RowShape<512, 1>());
+  else if (H <= 1024 * 8) f(RowShape<512, 2>());
   else if (H <= 2048 * 8) f(RowShape<1024, 2>());
   else f(RowShape<1024, 4>());
 }
 
 template <int XT, int YT>
-void launch_forward(const NormArgs& a, hipStream_t s) {
-  by_row_shape(a.H, [&](auto shape) {
-    using S = decltype(shape);
-    rmsnorm_kernel<XT, YT, S::TPR, S::RUNS><<<(uint32_t)((a.T + S::ROWS - 1) / S::ROWS), norm_threads(S::TPR), 0, s>>>(a);
-  });
+void launch_forward(const NormArgs& all, hipStream_t s) {
+  // (a launch holds fewer than 2^32 threads)
+  constexpr int64_t kPiece = int64_t(1) << 21;
+  for (int64_t t0 = 0; t0 < all.T; t0 += kPiece) {
+    NormArgs a = all;
+    a.T = all.T - t0 < kPiece ? all.T - t0 : kPiece;
+    a.x = elem_at(all.x, t0 * all.ldx, elem_bytes(XT));
+    if (all.r) a.r = elem_at(all.r, t0 * all.ldr, elem_bytes(XT));
+    if (all.sum) a.sum = elem_at(all.sum, t0 * all.lds, elem_bytes(XT));
+    a.y = elem_at(all.y, t0 * all.ldy, elem_bytes(YT));
+    a.scales = elem_at(all.scales, t0 * ((all.H + 127) / 128), all.e8m0 ? 1 : 4);
+    by_row_shape(a.H, [&](auto shape) {
+      using S = decltype(shape);
+      if (S::TPR == 64) rmsnorm_kernel<XT, YT, S::TPR, S::RUNS, S::SHORT><<<(uint32_t)((a.T + 3) / 4), 256, 0, s>>>(a);
+      else rmsnorm_kernel<XT, YT, S::TPR, S::RUNS, S::SHORT><<<(uint32_t)a.T, S::TPR, 0, s>>>(a);
+    });
+  }
 }
 
 hipError_t launch_rmsnorm(const NormArgs& a, hipStream_t s) {
@@ -211,11 +234,12 @@ hipError_t launch_rmsnorm(const NormArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Workgroups of the backward kernel.
+// Workgroups of the backward kernel: two for every compute unit, and one where it has at most two turns to make (a second launch costs more than they do).
 static int64_t backward_groups(int64_t T, int64_t H) {
-  const int rows = H <= 1024 ? 4 : 1;
-  const int64_t most = H <= 8192 ? 512 : 256, n = (T + rows - 1) / rows;
-  return n < most ? n : most;
+  int rows = 1;
+  by_row_shape((int)H, [&](auto shape) { rows = decltype(shape)::ROWS; });
+  const int64_t n = (T + rows - 1) / rows;
+  return n <= 2 ? (n ? 1 : 0) : n < 512 ? n : 512;
 }
 int64_t rmsnorm_workspace_words(int64_t T, int64_t H) {
   const int64_t n = backward_groups(T, H);
@@ -226,7 +250,7 @@ template <int XT, int YT>
 void launch_backward(const NormArgs& a, uint32_t groups, hipStream_t s) {
   by_row_shape(a.H, [&](auto shape) {
     using S = decltype(shape);
-    rmsnorm_backward_kernel<XT, YT, S::TPR, S::RUNS><<<groups, norm_threads(S::TPR), (S::ROWS - 1) * S::TPR * S::RUNS * 8 * 4, s>>>(a);
+    rmsnorm_backward_kernel<XT, YT, S::TPR, S::RUNS, S::ROWS, S::SHORT><<<groups, S::TPR * S::ROWS, (S::ROWS - 1) * S::TPR * S::RUNS * 8 * 4, s>>>(a);
   });
 }
 

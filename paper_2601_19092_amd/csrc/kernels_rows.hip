@@ -1,4 +1,8 @@
 // The tokens' rows in the experts' order and back (axe_rows_dispatch, axe_rows_combine, axe_rows_combine_backward).  gfx950 only.
+//
+// All three are bound by memory.  A wave takes 512 columns of a token, eight a lane (of a pair in the gradient, whose dot product wants the whole row): columns are
+// independent, so there is nothing to wait for but the memory, and a run of 128 columns that shares a scale is 16 neighbouring lanes.  dispatch
+// reads a token once and stores its k copies from registers; combine has the loads of eight rows in flight.
 #include <hip/hip_runtime.h>
 
 #include "layer_ops.h"
@@ -6,95 +10,239 @@
 
 namespace axe {
 
-// The row of a token's j-th choice, or -1.
-__device__ __forceinline__ int64_t row_at(const RowsArgs& a, int64_t t, int j) {
-  if (!a.row_of) return t;
-  const int64_t r = a.row_of[t * a.k + j];
-  return r >= 0 && r < a.M ? r : -1;
-}
+constexpr int kSlab = 512;                                         // columns of a wave
 
-// One workgroup per token.
-__global__ __launch_bounds__(256) void rows_dispatch_kernel(RowsArgs a) {
-  const int64_t t = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63, blocks = (a.H + 127) / 128;
-  if (a.t_type == a.r_type) {
-    const int eb = elem_bytes(a.t_type);
-    for (int j = 0; j < a.k; ++j) {
-      const int64_t r = row_at(a, t, j);
-      if (r < 0) continue;
-      for (int64_t c = tid; c < a.H; c += 256) {
-        if (eb == 1) ((uint8_t*)a.to_rows)[r * a.ldr + c] = ((const uint8_t*)a.tokens)[t * a.ldt + c];
-        else if (eb == 2) ((uint16_t*)a.to_rows)[r * a.ldr + c] = ((const uint16_t*)a.tokens)[t * a.ldt + c];
-        else ((uint32_t*)a.to_rows)[r * a.ldr + c] = ((const uint32_t*)a.tokens)[t * a.ldt + c];
-      }
-      if (eb == 1)
-        for (int b = tid; b < blocks; b += 256) {
-          if (a.e8m0) ((uint8_t*)a.scales)[r * blocks + b] = ((const uint8_t*)a.token_scales)[t * blocks + b];
-          else ((uint32_t*)a.scales)[r * blocks + b] = ((const uint32_t*)a.token_scales)[t * blocks + b];
-        }
-    }
-    return;
+// A token's rows: lane j holds the row of choice j (-1: none).
+struct RowsOf {
+  int mine;
+  __device__ __forceinline__ RowsOf(const RowsArgs& a, int64_t t, int lane) {
+    mine = -1;
+    if (!a.row_of) mine = (int)t;
+    else if (lane < a.k) mine = a.row_of[t * a.k + lane];
+    if (mine < 0 || mine >= a.M) mine = -1;
   }
-  for (int b = tid >> 6; b < blocks; b += 4) {                     // a wave per 128 columns
-    const int64_t c0 = b * 128 + lane, c1 = c0 + 64;
-    const float y0 = c0 < a.H ? load_elem(a.tokens, t * a.ldt + c0, a.t_type) : 0.0f, y1 = c1 < a.H ? load_elem(a.tokens, t * a.ldt + c1, a.t_type) : 0.0f;
-    float most = fmaxf(fabsf(y0), fabsf(y1));
-    for (int d = 32; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-    const Scale s = scale_of(fmaxf(most, 0.0f), a.e8m0);
-    const uint32_t q = pack_e4m3(y0 * s.inv, y1 * s.inv, 0, 0);
-    for (int j = 0; j < a.k; ++j) {
-      const int64_t r = row_at(a, t, j);
-      if (r < 0) continue;
-      if (c0 < a.H) ((uint8_t*)a.to_rows)[r * a.ldr + c0] = (uint8_t)q;
-      if (c1 < a.H) ((uint8_t*)a.to_rows)[r * a.ldr + c1] = (uint8_t)(q >> 8);
-      if (lane) continue;
-      if (a.e8m0) ((uint8_t*)a.scales)[r * blocks + b] = (uint8_t)s.code;
-      else ((float*)a.scales)[r * blocks + b] = s.s;
-    }
+  __device__ __forceinline__ int row(int j) const { return __builtin_amdgcn_readlane(mine, j); }
+};
+// Which token and which columns a wave has.
+struct WaveAt {
+  int lane, c;
+  int64_t t;
+  bool there;
+  __device__ __forceinline__ WaveAt(int64_t T, int H) {
+    const int slabs = (H + kSlab - 1) / kSlab;
+    const uint32_t w = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lane = threadIdx.x & 63;
+    t = w / (uint32_t)slabs;
+    c = (int)(w - (uint32_t)t * slabs) * kSlab + lane * 8;
+    there = t < T;
+  }
+};
+
+// Copies of elements of TYPE's size (fp32 as pairs of 16 bits).
+template <int TYPE, bool SHORT>
+__global__ __launch_bounds__(256) void rows_copy_kernel(RowsArgs a, int H, int64_t ldt, int64_t ldr) {
+  const WaveAt w(a.T, H);
+  if (!w.there) return;
+  constexpr int EB = elem_bytes(TYPE);
+  Run8<TYPE> v;
+  load_run<SHORT>(v, elem_at(a.tokens, w.t * ldt, EB), w.c, H);
+  const RowsOf rows(a, w.t, w.lane);
+  end_run<SHORT>(v, w.c, H);
+  for (int j = 0; j < a.k; ++j) {
+    const int64_t r = rows.row(j);
+    if (r >= 0) store_run(v, elem_at(a.to_rows, r * ldr, EB), w.c, H);
   }
 }
+// The scales of e4m3 tokens to their rows: a thread per pair and scale.
+template <class S>
+__global__ __launch_bounds__(256) void rows_copy_scales_kernel(RowsArgs a, int blocks) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, pair = i / blocks;
+  if (pair >= a.T * a.k) return;
+  const int b = (int)(i - pair * blocks);
+  const int64_t t = pair / a.k, r = a.row_of ? a.row_of[pair] : t;
+  if (r >= 0 && r < a.M) ((S*)a.scales)[r * blocks + b] = ((const S*)a.token_scales)[t * blocks + b];
+}
 
+template <int TYPE, bool SHORT>
+__global__ __launch_bounds__(256) void rows_quantise_kernel(RowsArgs a) {
+  const WaveAt w(a.T, a.H);
+  if (!w.there) return;
+  Run8<TYPE> v;
+  load_run<SHORT>(v, elem_at(a.tokens, w.t * a.ldt, elem_bytes(TYPE)), w.c, a.H);
+  const RowsOf rows(a, w.t, w.lane);
+  end_run<SHORT>(v, w.c, a.H);
+  float y[8], most = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) y[k] = v.get(k), most = fmaxf(most, fabsf(y[k]));
+  const Scale s = scale_of(row16_all<Max>(most), a.e8m0);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) y[k] *= s.inv;
+  Run8<kFp8> q;
+  q.set(y);
+  const int blocks = (a.H + 127) >> 7;
+  for (int j = 0; j < a.k; ++j) {
+    const int64_t r = rows.row(j);
+    if (r < 0) continue;
+    store_run(q, elem_at(a.to_rows, r * a.ldr, 1), w.c, a.H);
+    if ((w.lane & 15) == 0 && w.c < a.H) store_scale(a.scales, r * blocks + (w.c >> 7), s, a.e8m0);
+  }
+}
+
+template <int TYPE, bool SHORT>
 __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
-  const int64_t t = blockIdx.x;
-  for (int64_t c = threadIdx.x; c < a.H; c += 256) {
-    float v = a.add ? load_elem(a.add, t * a.ldt + c, a.t_type) : 0.0f;
-    for (int j = 0; j < a.k; ++j) {
-      const int64_t r = row_at(a, t, j);
-      if (r >= 0) v += (a.weights ? a.weights[t * a.k + j] : 1.0f) * load_elem(a.rows, r * a.ldr + c, a.r_type);
+  const WaveAt w(a.T, a.H);
+  if (!w.there) return;
+  constexpr int EB = elem_bytes(TYPE);
+  const RowsOf rows(a, w.t, w.lane);
+  const float weight = a.weights && w.lane < a.k ? a.weights[w.t * a.k + w.lane] : 1.0f;
+  float sum[8];
+  Run8<TYPE> v;
+  v.clear();
+  if (a.add) load_run<SHORT>(v, elem_at(a.add, w.t * a.ldt, EB), w.c, a.H), end_run<SHORT>(v, w.c, a.H);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum[k] = v.get(k);
+  for (int j0 = 0; j0 < a.k; j0 += 8) {
+    Run8<TYPE> c[8];
+    int r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      r[j] = j0 + j < a.k ? rows.row(j0 + j) : -1;
+      if (r[j] >= 0) load_run<SHORT>(c[j], elem_at(a.rows, r[j] * a.ldr, EB), w.c, a.H);
     }
-    store_elem(a.to_tokens, t * a.ldt + c, a.t_type, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (r[j] < 0) continue;
+      end_run<SHORT>(c[j], w.c, a.H);
+      const float wj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight), j0 + j));
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum[k] += wj * c[j].get(k);
+    }
   }
+  v.set(sum);
+  store_run(v, elem_at(a.to_tokens, w.t * a.ldt, EB), w.c, a.H);
 }
 
-// One workgroup per pair.
+// A wave per pair.
+template <int TYPE, bool SHORT>
 __global__ __launch_bounds__(256) void rows_combine_backward_kernel(RowsArgs a) {
-  __shared__ float lds[4];
-  const int64_t pair = blockIdx.x, t = pair / a.k;
-  const int64_t r = row_at(a, t, (int)(pair - t * a.k));
+  constexpr int EB = elem_bytes(TYPE), RUNS = SHORT ? 1 : 4;
+  const int lane = threadIdx.x & 63;
+  const int64_t pair = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (pair >= a.T * a.k) return;
+  const int64_t t = pair / a.k;
+  const int64_t r = a.row_of[pair];
   float dot = 0;
-  if (r >= 0) {
+  if (r >= 0 && r < a.M) {
     const float w = a.weights ? a.weights[pair] : 1.0f;
-    for (int64_t c = threadIdx.x; c < a.H; c += 256) {
-      const float d = load_elem(a.tokens, t * a.ldt + c, a.t_type);
-      if (a.rows) dot += d * load_elem(a.rows, r * a.ldr + c, a.r_type);
-      if (a.to_rows) store_elem(a.to_rows, r * a.ldr + c, a.r_type, w * d);
+    const void *rd = elem_at(a.tokens, t * a.ldt, EB), *rc = elem_at(a.rows, r * a.ldr, EB);
+    void* ro = elem_at(a.to_rows, r * a.ldr, EB);
+    for (int c0 = 0; c0 < a.H; c0 += kSlab * RUNS) {
+      Run8<TYPE> d[RUNS], c[RUNS];
+#pragma unroll
+      for (int i = 0; i < RUNS; ++i) {
+        if (c0 + i * kSlab >= a.H) break;
+        load_run<SHORT>(d[i], rd, c0 + i * kSlab + lane * 8, a.H);
+        if (a.rows) load_run<SHORT>(c[i], rc, c0 + i * kSlab + lane * 8, a.H);
+      }
+#pragma unroll
+      for (int i = 0; i < RUNS; ++i) {
+        const int ci = c0 + i * kSlab + lane * 8;
+        if (c0 + i * kSlab >= a.H) break;
+        end_run<SHORT>(d[i], ci, a.H);
+        if (a.rows) {
+          end_run<SHORT>(c[i], ci, a.H);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) dot += d[i].get(k) * c[i].get(k);
+        }
+        if (a.to_rows) {
+          float v[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = w * d[i].get(k);
+          d[i].set(v);
+          store_run(d[i], ro, ci, a.H);
+        }
+      }
     }
+    dot = wave_sum(dot);
   }
-  dot = group_sum<4>(dot, lds);
-  if (a.dweights && threadIdx.x == 0) a.dweights[pair] = dot;
+  if (a.dweights && lane == 0) a.dweights[pair] = dot;
 }
 
+// A launch holds fewer than 2^32 threads: calls of more waves go in pieces of whole tokens.
+template <class F>
+hipError_t in_pieces(const RowsArgs& a, int64_t waves_per_token, F&& f) {
+  const int64_t most = ((int64_t)1 << 25) / waves_per_token, piece = most ? most : 1;
+  for (int64_t t0 = 0; t0 < a.T; t0 += piece) {
+    RowsArgs p = a;
+    p.T = a.T - t0 < piece ? a.T - t0 : piece;
+    const int64_t blocks = (a.H + 127) / 128;
+    p.tokens = elem_at(a.tokens, t0 * a.ldt, elem_bytes(a.t_type)), p.to_tokens = elem_at(a.to_tokens, t0 * a.ldt, elem_bytes(a.t_type));
+    p.token_scales = elem_at(a.token_scales, t0 * blocks, a.e8m0 ? 1 : 4);
+    if (a.add) p.add = elem_at(a.add, t0 * a.ldt, elem_bytes(a.t_type));
+    if (a.row_of) p.row_of = a.row_of + t0 * a.k;
+    else p.to_rows = elem_at(a.to_rows, t0 * a.ldr, elem_bytes(a.r_type)), p.scales = elem_at(a.scales, t0 * blocks, a.e8m0 ? 1 : 4), p.M = p.T;
+    if (a.weights) p.weights = a.weights + t0 * a.k;
+    if (a.dweights) p.dweights = a.dweights + t0 * a.k;
+    f(p, (uint32_t)((p.T * waves_per_token + 3) / 4));
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+static int64_t slabs_of(int64_t columns) { return (columns + kSlab - 1) / kSlab; }
+
+template <int TYPE>
+void launch_quantise(const RowsArgs& p, uint32_t groups, hipStream_t s) {
+  if (p.H < 8) rows_quantise_kernel<TYPE, true><<<groups, 256, 0, s>>>(p);
+  else rows_quantise_kernel<TYPE, false><<<groups, 256, 0, s>>>(p);
+}
 hipError_t launch_rows_dispatch(const RowsArgs& a, hipStream_t s) {
-  rows_dispatch_kernel<<<(uint32_t)a.T, 256, 0, s>>>(a);
-  return hipGetLastError();
+  if (a.t_type != a.r_type)
+    return in_pieces(a, slabs_of(a.H), [&](const RowsArgs& p, uint32_t groups) {
+      if (a.t_type == kBf16) launch_quantise<kBf16>(p, groups, s);
+      else if (a.t_type == kF16) launch_quantise<kF16>(p, groups, s);
+      else launch_quantise<kF32>(p, groups, s);
+    });
+  // as 16-bit elements, but e4m3 whose rows are odd or start anywhere
+  const int eb = elem_bytes(a.t_type);
+  const bool bytes = eb == 1 && ((a.H | a.ldt | a.ldr | (int64_t)(uintptr_t)a.tokens | (int64_t)(uintptr_t)a.to_rows) & 1);
+  const int n = bytes ? a.H : a.H * eb / 2;
+  const int64_t scale_waves = a.t_type == kFp8 ? (int64_t)a.k * ((a.H + 127) / 128) / 64 + 1 : 0, slabs = slabs_of(n);
+  return in_pieces(a, slabs > scale_waves ? slabs : scale_waves, [&](const RowsArgs& p, uint32_t) {
+    const uint32_t groups = (uint32_t)((p.T * slabs + 3) / 4);
+    const int64_t ldt = bytes ? p.ldt : p.ldt * eb / 2, ldr = bytes ? p.ldr : p.ldr * eb / 2;
+    if (bytes && n < 8) rows_copy_kernel<kFp8, true><<<groups, 256, 0, s>>>(p, n, ldt, ldr);
+    else if (bytes) rows_copy_kernel<kFp8, false><<<groups, 256, 0, s>>>(p, n, ldt, ldr);
+    else if (n < 8) rows_copy_kernel<kBf16, true><<<groups, 256, 0, s>>>(p, n, ldt, ldr);
+    else rows_copy_kernel<kBf16, false><<<groups, 256, 0, s>>>(p, n, ldt, ldr);
+    if (a.t_type == kFp8) {
+      const int blocks = (a.H + 127) / 128;
+      const uint32_t sg = (uint32_t)((p.T * p.k * blocks + 255) / 256);
+      if (a.e8m0) rows_copy_scales_kernel<uint8_t><<<sg, 256, 0, s>>>(p, blocks);
+      else rows_copy_scales_kernel<uint32_t><<<sg, 256, 0, s>>>(p, blocks);
+    }
+  });
+}
+
+template <int TYPE>
+hipError_t launch_combine(const RowsArgs& a, hipStream_t s) {
+  return in_pieces(a, slabs_of(a.H), [&](const RowsArgs& p, uint32_t groups) {
+    if (a.H < 8) rows_combine_kernel<TYPE, true><<<groups, 256, 0, s>>>(p);
+    else rows_combine_kernel<TYPE, false><<<groups, 256, 0, s>>>(p);
+  });
 }
 hipError_t launch_rows_combine(const RowsArgs& a, hipStream_t s) {
-  rows_combine_kernel<<<(uint32_t)a.T, 256, 0, s>>>(a);
-  return hipGetLastError();
+  return a.r_type == kBf16 ? launch_combine<kBf16>(a, s) : a.r_type == kF16 ? launch_combine<kF16>(a, s) : launch_combine<kF32>(a, s);
+}
+
+template <int TYPE>
+hipError_t launch_combine_backward(const RowsArgs& a, hipStream_t s) {
+  return in_pieces(a, a.k, [&](const RowsArgs& p, uint32_t groups) {
+    if (a.H < 8) rows_combine_backward_kernel<TYPE, true><<<groups, 256, 0, s>>>(p);
+    else rows_combine_backward_kernel<TYPE, false><<<groups, 256, 0, s>>>(p);
+  });
 }
 hipError_t launch_rows_combine_backward(const RowsArgs& a, hipStream_t s) {
-  rows_combine_backward_kernel<<<(uint32_t)(a.T * a.k), 256, 0, s>>>(a);
-  return hipGetLastError();
+  return a.r_type == kBf16 ? launch_combine_backward<kBf16>(a, s) : a.r_type == kF16 ? launch_combine_backward<kF16>(a, s) : launch_combine_backward<kF32>(a, s);
 }
 
 }  // namespace axe

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "layer_ops.h"
 
 namespace axe {
@@ -43,8 +45,30 @@ struct Run8<kBf16> {
       b[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});    // round to nearest even
     }
   }
-  __device__ __forceinline__ Elem elem(int i) const { return (Elem)(b[i >> 1] >> (i & 1) * 16); }
-  __device__ __forceinline__ void put(int i, Elem e) { b[i >> 1] = i & 1 ? (b[i >> 1] & 0xffffu) | (uint32_t)e << 16 : (b[i >> 1] & 0xffff0000u) | e; }
+  // the run moved down by n elements, zeros behind (0 <= n <= 8)
+  __device__ __forceinline__ void down(int n) {
+    const uint32_t h = (n & 1) * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = (uint32_t)(((uint64_t)(i < 3 ? b[i + 1] : 0) << 32 | b[i]) >> h);
+    b = n & 2 ? u32x4{b[1], b[2], b[3], 0} : b;
+    b = n & 4 ? u32x4{b[2], b[3], 0, 0} : b;
+    b = n & 8 ? u32x4{} : b;
+  }
+  __device__ __forceinline__ void load_part(const Elem* p, int n) {
+    clear();
+    if (n & 4) {
+      const u32x2 v = load_bits<u32x2>(p);
+      b[0] = v[0], b[1] = v[1];
+    }
+    if (n & 2) b[n & 4 ? 2 : 0] = load_bits<uint32_t>(p + (n & 4));
+    if (n & 1) b[n >> 1] = p[n & 6];
+  }
+  __device__ __forceinline__ void store_part(Elem* p, int n) const {
+    Run8 r = *this;
+    if (n & 4) store_bits(p, u32x2{r.b[0], r.b[1]}), p += 4, r.down(4);
+    if (n & 2) store_bits(p, r.b[0]), p += 2, r.down(2);
+    if (n & 1) *p = (Elem)r.b[0];
+  }
 };
 template <>
 struct Run8<kF16> {
@@ -61,8 +85,30 @@ struct Run8<kF16> {
       b[i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)v[2 * i], (_Float16)v[2 * i + 1]});
     }
   }
-  __device__ __forceinline__ Elem elem(int i) const { return (Elem)(b[i >> 1] >> (i & 1) * 16); }
-  __device__ __forceinline__ void put(int i, Elem e) { b[i >> 1] = i & 1 ? (b[i >> 1] & 0xffffu) | (uint32_t)e << 16 : (b[i >> 1] & 0xffff0000u) | e; }
+  // the run moved down by n elements, zeros behind (0 <= n <= 8)
+  __device__ __forceinline__ void down(int n) {
+    const uint32_t h = (n & 1) * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = (uint32_t)(((uint64_t)(i < 3 ? b[i + 1] : 0) << 32 | b[i]) >> h);
+    b = n & 2 ? u32x4{b[1], b[2], b[3], 0} : b;
+    b = n & 4 ? u32x4{b[2], b[3], 0, 0} : b;
+    b = n & 8 ? u32x4{} : b;
+  }
+  __device__ __forceinline__ void load_part(const Elem* p, int n) {
+    clear();
+    if (n & 4) {
+      const u32x2 v = load_bits<u32x2>(p);
+      b[0] = v[0], b[1] = v[1];
+    }
+    if (n & 2) b[n & 4 ? 2 : 0] = load_bits<uint32_t>(p + (n & 4));
+    if (n & 1) b[n >> 1] = p[n & 6];
+  }
+  __device__ __forceinline__ void store_part(Elem* p, int n) const {
+    Run8 r = *this;
+    if (n & 4) store_bits(p, u32x2{r.b[0], r.b[1]}), p += 4, r.down(4);
+    if (n & 2) store_bits(p, r.b[0]), p += 2, r.down(2);
+    if (n & 1) *p = (Elem)r.b[0];
+  }
 };
 template <>
 struct Run8<kF32> {
@@ -76,8 +122,28 @@ struct Run8<kF32> {
 #pragma unroll
     for (int i = 0; i < 8; ++i) b[i >> 2][i & 3] = __float_as_uint(v[i]);
   }
-  __device__ __forceinline__ Elem elem(int i) const { return b[i >> 2][i & 3]; }
-  __device__ __forceinline__ void put(int i, Elem e) { b[i >> 2][i & 3] = e; }
+  __device__ __forceinline__ void down(int n) {
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t up = i + d < 8 ? b[(i + d) >> 2][(i + d) & 3] : 0;
+        b[i >> 2][i & 3] = n & d ? up : b[i >> 2][i & 3];
+      }
+    if (n & 8) clear();
+  }
+  __device__ __forceinline__ void load_part(const Elem* p, int n) {
+    clear();
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+      if (i < n) b[i >> 2][i & 3] = p[i];
+  }
+  __device__ __forceinline__ void store_part(Elem* p, int n) const {
+    Run8 r = *this;
+    if (n & 4) store_bits(p, r.b[0]), p += 4, r.down(4);
+    if (n & 2) store_bits(p, u32x2{r.b[0][0], r.b[0][1]}), p += 2, r.down(2);
+    if (n & 1) *p = r.b[0][0];
+  }
 };
 template <>
 struct Run8<kFp8> {
@@ -87,57 +153,68 @@ struct Run8<kFp8> {
   __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x2>(p); }
   __device__ __forceinline__ void store(void* p) const { store_bits(p, b); }
   __device__ __forceinline__ void set(const float (&v)[8]);
-  __device__ __forceinline__ Elem elem(int i) const { return (Elem)(b[i >> 2] >> (i & 3) * 8); }
-  __device__ __forceinline__ void put(int i, Elem e) { b[i >> 2] = (b[i >> 2] & ~(0xffu << (i & 3) * 8)) | (uint32_t)e << (i & 3) * 8; }
+  __device__ __forceinline__ void down(int n) {
+    const uint64_t v = n < 8 ? ((uint64_t)b[1] << 32 | b[0]) >> n * 8 : 0;
+    b = u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
+  }
+  __device__ __forceinline__ void load_part(const Elem* p, int n) {
+    uint64_t v = 0;
+    for (int i = 0; i < n; ++i) v |= (uint64_t)p[i] << i * 8;
+    b = u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
+  }
+  __device__ __forceinline__ void store_part(Elem* p, int n) const {
+    Run8 r = *this;
+    if (n & 4) store_bits(p, r.b[0]), p += 4, r.down(4);
+    if (n & 2) store_bits(p, (uint16_t)r.b[0]), p += 2, r.down(2);
+    if (n & 1) *p = (Elem)r.b[0];
+  }
 };
 
-// The run at element i of a row, `left` elements before its end (none: zeros, nothing read).
-template <int TYPE>
-__device__ __forceinline__ void load_run(Run8<TYPE>& r, const void* row, int64_t i, int left) {
+// The run at element i of a row of H elements, in two steps; what lies past the row's end comes out as zero.  A run that would reach past the end (or lies behind
+// it) is read as the row's last eight elements and moved down in the second step: the loads of all threads are then single instructions with no branch
+// around them, and all of a thread's can be in flight.  Rows of fewer than eight elements (SHORT) are put together from what they have.
+template <bool SHORT, int TYPE>
+__device__ __forceinline__ void load_run(Run8<TYPE>& r, const void* row, int i, int H) {
   using E = typename Run8<TYPE>::Elem;
-  const E* p = (const E*)row + i;
-  if (left >= 8) {
-    r.load(p);
-    return;
-  }
-  r.clear();
-#pragma unroll
-  for (int k = 0; k < 7; ++k)
-    if (k < left) r.put(k, p[k]);
+  if (SHORT) r.load_part((const E*)row, i == 0 ? H : 0);
+  else r.load((const E*)row + (i + 8 <= H ? i : H - 8));
+}
+template <bool SHORT, int TYPE>
+__device__ __forceinline__ void end_run(Run8<TYPE>& r, int i, int H) {
+  if (!SHORT && i + 8 > H) r.down(i < H ? i + 8 - H : 8);
 }
 template <int TYPE>
-__device__ __forceinline__ void store_run(const Run8<TYPE>& r, void* row, int64_t i, int left) {
+__device__ __forceinline__ void store_run(const Run8<TYPE>& r, void* row, int i, int H) {
   using E = typename Run8<TYPE>::Elem;
-  E* p = (E*)row + i;
-  if (left >= 8) {
-    r.store(p);
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < 7; ++k)
-    if (k < left) p[k] = r.elem(k);
+  if (i + 8 <= H) r.store((E*)row + i);
+  else if (i < H) r.store_part((E*)row + i, H - i);
 }
-// Weights of a type known at run time, as fp32; null: ones.
-__device__ __forceinline__ void load_weights(float (&w)[8], const void* p, int type, int64_t i, int left) {
+template <class E>
+__host__ __device__ __forceinline__ E* elem_at(E* p, int64_t i, int bytes) { return (E*)((std::conditional_t<std::is_const<E>::value, const char, char>*)p + i * bytes); }
+
+// RUNS runs of weights, TPR * 8 columns apart, of a type known at run time; null: ones (past the end: anything, it meets zeros).
+template <bool SHORT, int TPR, int RUNS, int TYPE>
+__device__ __forceinline__ void weights_of(float (&w)[RUNS][8], const void* p, int c, int H) {
+  Run8<TYPE> r[RUNS];
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i) load_run<SHORT>(r[i], p, c + i * TPR * 8, H);
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i) {
+    end_run<SHORT>(r[i], c + i * TPR * 8, H);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[i][k] = r[i].get(k);
+  }
+}
+template <bool SHORT, int TPR, int RUNS>
+__device__ __forceinline__ void load_weights(float (&w)[RUNS][8], const void* p, int type, int c, int H) {
   if (!p) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = 1.0f;
-  } else if (type == kF32) {
-    Run8<kF32> r;
-    load_run(r, p, i, left);
+    for (int i = 0; i < RUNS; ++i)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = r.get(k);
-  } else if (type == kBf16) {
-    Run8<kBf16> r;
-    load_run(r, p, i, left);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = r.get(k);
-  } else {
-    Run8<kF16> r;
-    load_run(r, p, i, left);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = r.get(k);
-  }
+      for (int k = 0; k < 8; ++k) w[i][k] = 1.0f;
+  } else if (type == kF32) weights_of<SHORT, TPR, RUNS, kF32>(w, p, c, H);
+  else if (type == kBf16) weights_of<SHORT, TPR, RUNS, kBf16>(w, p, c, H);
+  else weights_of<SHORT, TPR, RUNS, kF16>(w, p, c, H);
 }
 
 // Exchanges inside a row of 16 lanes are operands of the instruction that uses them (DPP); between rows gfx950 swaps whole rows.
@@ -168,16 +245,16 @@ __device__ __forceinline__ float wave_all(float v) {
   return OP::of(__int_as_float(b[0]), __int_as_float(b[1]));
 }
 __device__ __forceinline__ float wave_sum(float v) { return wave_all<Add>(v); }
-// The sums of N values over the threads of a row that WAVES waves hold, in every thread.  lds: N x WAVES floats of the row; what was read from it before a
-// barrier may be overwritten.
+// The sums of N values over the threads of a row that WAVES waves hold, in every thread; wave: which of them this is.  lds: N x WAVES floats of the row, which
+// the caller does not reuse before another barrier.
 template <int N, int WAVES>
-__device__ __forceinline__ void row_sums(float (&v)[N], float* lds) {
+__device__ __forceinline__ void row_sums(float (&v)[N], float* lds, int wave) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
   if (WAVES == 1) return;
   if ((threadIdx.x & 63) == 0)
 #pragma unroll
-    for (int i = 0; i < N; ++i) lds[i * WAVES + (threadIdx.x >> 6)] = v[i];
+    for (int i = 0; i < N; ++i) lds[i * WAVES + wave] = v[i];
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
