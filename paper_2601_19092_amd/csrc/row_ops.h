@@ -10,11 +10,6 @@
 
 namespace axe {
 
-// One element, of a type known at run time only.
-__device__ __forceinline__ float load_elem(const void* p, int64_t i, int type) {
-  return type == kBf16 ? (float)((const __bf16*)p)[i] : type == kF16 ? (float)((const _Float16*)p)[i] : ((const float*)p)[i];
-}
-
 // Eight neighbouring elements of a row, as bits: 16 bytes in 16-bit types, 32 in fp32, 8 in e4m3.  The kernels give every thread such runs.  They may start at any
 // element: the hardware takes 16-byte accesses at any address, so rows of odd pitches need no path of their own, they only touch more lines.
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
