@@ -212,14 +212,15 @@ class Layout:
 _torch = None                                                      # the torch module, once a call has needed it
 _raw_stream = None
 _device = None
+_I32 = _F32 = None                                                 # its types
 
 
 def _need_torch():
-    global _torch, _raw_stream, _device
+    global _torch, _raw_stream, _device, _I32, _F32
     import torch
     _device = getattr(torch._C, "_cuda_getDevice", None)
     _raw_stream = _device is not None and getattr(torch._C, "_cuda_getCurrentRawStream", False)
-    _torch = torch
+    _torch, _I32, _F32 = torch, torch.int32, torch.float32
     return torch
 
 
@@ -440,11 +441,19 @@ def _ptr(t, elems: int = 0):
     return t.data_ptr()
 
 
-def _flat(t, elems: int, dtype: str):
-    """The same of an array without a layout: contiguous, of one type."""
+def _ints(t, elems: int):
+    """The same of an array without a layout: contiguous, of 32-bit integers."""
     if t is None:
         return None
-    assert t.is_cuda and t.is_contiguous() and t.numel() >= elems and str(t.dtype) == dtype, f"{elems} contiguous elements of {dtype} on the device"
+    assert t.is_cuda and t.is_contiguous() and t.numel() >= elems and t.dtype is (_I32 or _need_torch().int32), "contiguous int32 elements on the device, as many as the call touches"
+    return t.data_ptr()
+
+
+def _floats(t, elems: int):
+    """... of fp32."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.is_contiguous() and t.numel() >= elems and t.dtype is (_F32 or _need_torch().float32), "contiguous fp32 elements on the device, as many as the call touches"
     return t.data_ptr()
 
 
@@ -483,7 +492,7 @@ def axe_rmsnorm_backward(desc: RmsNormDesc, dy, sum, weight, dx, dsum=None, dwei
     """Gradients of x (and of residual) and, with dweight, of the weights; `sum` is the normed rows, dsum what arrives at them otherwise."""
     ex, er, es, ey = desc.elems
     rc = (_lib or lib()).axe_rmsnorm_backward(desc.ref, _ptr(dy, ey), _ptr(sum, es), _ptr(weight, desc.c.H), _ptr(dsum, er), _ptr(dx, ex),
-                                              _flat(dweight, desc.c.H, "torch.float32"), *_words(workspace), _stream_ptr(stream))
+                                              _floats(dweight, desc.c.H), *_words(workspace), _stream_ptr(stream))
     if rc:
         _check(rc)
     return dx
@@ -498,14 +507,14 @@ class RouteDesc:
         L, n = _matrix(logits, T, E, logits_elems, mem_axis)
         self.layouts, self.bias, self.elems, self.pairs = (L,), bias, n, T * k
         self.c = axe_route_desc_t(T, E, k, logit_dtype, score, int(bool(renorm)), groups, groups_kept, group_score, scale, L.axis(mem_axis), L.c, n,
-                                  _flat(bias, E, "torch.float32"))
+                                  _floats(bias, E))
         self.ref = C.byref(self.c)
 
 
 def axe_route(desc: RouteDesc, logits, ids, weights, group_rows=None, row_of=None, workspace=None, stream=None):
     """Chosen experts (int32) and weights (fp32) of every token; group_rows (int32, E + 1) and row_of (int32, as ids): the experts' order of the pairs."""
-    rc = (_lib or lib()).axe_route(desc.ref, _ptr(logits, desc.elems), _flat(ids, desc.pairs, "torch.int32"), _flat(weights, desc.pairs, "torch.float32"),
-                                   _flat(group_rows, desc.c.E + 1, "torch.int32"), _flat(row_of, desc.pairs, "torch.int32"), *_words(workspace), _stream_ptr(stream))
+    rc = (_lib or lib()).axe_route(desc.ref, _ptr(logits, desc.elems), _ints(ids, desc.pairs), _floats(weights, desc.pairs),
+                                   _ints(group_rows, desc.c.E + 1), _ints(row_of, desc.pairs), *_words(workspace), _stream_ptr(stream))
     if rc:
         _check(rc)
     return ids, weights
@@ -518,7 +527,7 @@ def axe_route_workspace(desc: RouteDesc) -> int:
 
 def axe_route_backward(desc: RouteDesc, logits, ids, dweights, dlogits, stream=None):
     """Gradient of the logits from that of the weights."""
-    rc = (_lib or lib()).axe_route_backward(desc.ref, _ptr(logits, desc.elems), _flat(ids, desc.pairs, "torch.int32"), _flat(dweights, desc.pairs, "torch.float32"),
+    rc = (_lib or lib()).axe_route_backward(desc.ref, _ptr(logits, desc.elems), _ints(ids, desc.pairs), _floats(dweights, desc.pairs),
                                             _ptr(dlogits, desc.elems), _stream_ptr(stream))
     if rc:
         _check(rc)
@@ -540,7 +549,7 @@ class RowsDesc:
 def axe_rows_dispatch(desc: RowsDesc, tokens, row_of, rows, token_scales=None, scales=None, stream=None):
     """rows[row_of[t][j]] = tokens[t], quantised where the rows are e4m3 (row_of None: the rows are in order already)."""
     nt, nr = desc.elems
-    rc = (_lib or lib()).axe_rows_dispatch(desc.ref, _ptr(tokens, nt), _ptr(token_scales, desc.c.T * desc.nb), _flat(row_of, desc.pairs, "torch.int32"), _ptr(rows, nr),
+    rc = (_lib or lib()).axe_rows_dispatch(desc.ref, _ptr(tokens, nt), _ptr(token_scales, desc.c.T * desc.nb), _ints(row_of, desc.pairs), _ptr(rows, nr),
                                            _ptr(scales, desc.c.M * desc.nb), _stream_ptr(stream))
     if rc:
         _check(rc)
@@ -550,7 +559,7 @@ def axe_rows_dispatch(desc: RowsDesc, tokens, row_of, rows, token_scales=None, s
 def axe_rows_combine(desc: RowsDesc, rows, row_of, weights, tokens, add=None, stream=None):
     """tokens[t] = add[t] + sum_j weights[t][j] rows[row_of[t][j]] (weights None: ones)."""
     nt, nr = desc.elems
-    rc = (_lib or lib()).axe_rows_combine(desc.ref, _ptr(rows, nr), _flat(row_of, desc.pairs, "torch.int32"), _flat(weights, desc.pairs, "torch.float32"), _ptr(add, nt),
+    rc = (_lib or lib()).axe_rows_combine(desc.ref, _ptr(rows, nr), _ints(row_of, desc.pairs), _floats(weights, desc.pairs), _ptr(add, nt),
                                           _ptr(tokens, nt), _stream_ptr(stream))
     if rc:
         _check(rc)
@@ -560,8 +569,8 @@ def axe_rows_combine(desc: RowsDesc, rows, row_of, weights, tokens, add=None, st
 def axe_rows_combine_backward(desc: RowsDesc, dtokens, rows, row_of, weights, drows=None, dweights=None, stream=None):
     """Gradients of the rows and of the weights from that of the tokens."""
     nt, nr = desc.elems
-    rc = (_lib or lib()).axe_rows_combine_backward(desc.ref, _ptr(dtokens, nt), _ptr(rows, nr), _flat(row_of, desc.pairs, "torch.int32"),
-                                                   _flat(weights, desc.pairs, "torch.float32"), _ptr(drows, nr), _flat(dweights, desc.pairs, "torch.float32"),
+    rc = (_lib or lib()).axe_rows_combine_backward(desc.ref, _ptr(dtokens, nt), _ptr(rows, nr), _ints(row_of, desc.pairs),
+                                                   _floats(weights, desc.pairs), _ptr(drows, nr), _floats(dweights, desc.pairs),
                                                    _stream_ptr(stream))
     if rc:
         _check(rc)

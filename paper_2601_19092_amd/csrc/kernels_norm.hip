@@ -15,6 +15,7 @@ template <int XT, int YT, int TPR, int RUNS, bool SHORT>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_kernel(NormArgs a) {
   constexpr int WAVES = TPR / 64, ROWS = TPR == 64 ? 4 : 1;
   __shared__ float lds[WAVES];
+  fetch_arguments(a.x, a.T, a.eps);
   const int c = threadIdx.x % TPR * 8;                             // column of the thread's first run
   const int64_t t = (int64_t)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
   if (t >= a.T) return;                                            // (whole waves of rows of one wave, or none)
@@ -81,6 +82,7 @@ __global__ __launch_bounds__(TPR * ROWS) void rmsnorm_backward_kernel(NormArgs a
   constexpr int WAVES = TPR / 64;
   __shared__ float lds[2][ROWS][2 * WAVES];
   extern __shared__ float part[];
+  fetch_arguments(a.x, a.T, a.eps);
   const int tid = threadIdx.x % TPR, c = tid * 8, sub = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
   float dw[RUNS][8] = {};
   int turn = 0;
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(TPR * ROWS) void rmsnorm_backward_kernel(NormArgs a
       for (int i = 0; i < RUNS; ++i)
 #pragma unroll
         for (int k = 0; k < 8; ++k) part[(sub - 1) * W + (i * 8 + k) * TPR + tid] = dw[i][k];
-    __syncthreads();
+    lds_barrier();
     if (sub > 0) return;
     for (int o = 0; o < ROWS - 1; ++o)
 #pragma unroll
@@ -172,7 +174,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_dweight_kernel(const float* ws, 
   for (int k = 0; k < 7; ++k)
     if (r + 16 * k < n) v[k] += ws[(int64_t)(r + 16 * k) * H + at];
   lds[wave][lane] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-  __syncthreads();
+  lds_barrier();
   if (wave) return;
   float s = 0;
 #pragma unroll

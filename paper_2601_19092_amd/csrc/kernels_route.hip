@@ -1,8 +1,8 @@
 // Routing of tokens to experts, the experts' order of the pairs, and the gradient of the logits (axe_route, axe_route_backward).  gfx950 only.
 //
 // A token's logits are a few hundred bytes, so what these calls cost is the launches and the chain of dependent steps behind each token, not memory.  A
-// token has 16 lanes (64 beyond 256 experts or 16 choices), each with 8 or 16 neighbouring experts in registers; k times its lanes agree on the largest choice (a maximum by DPP,
-// then the lowest index that has it) and its owner strikes it out.  Choices are compared as integers of the same order as the numbers.
+// token has 16 to 64 lanes, each with up to 16 neighbouring experts, sorted, in registers; k times its lanes agree on the largest choice (a maximum of their first ones by DPP,
+// then the first lane that has it), whose owner notes it down and moves its list up: some 170 ns each.  Choices are compared as integers of the same order as the numbers.
 //
 // The experts' order is a stable counting sort.  A workgroup has a block of consecutive tokens, 64 at a time, as bits of one 64-bit mask per expert in LDS: whatever the order
 // in which the bits arrive, the number of set bits below a token's is its place among the expert's pairs.  Up to 64 tokens are one workgroup, which goes on to add up the
@@ -22,12 +22,22 @@ constexpr int kNone = INT32_MIN;                                   // below ever
 
 // A logit as the formulas take it: NaN is a masked expert (-inf), +inf the largest number; -0 is 0.
 __device__ __forceinline__ float as_logit(float l) { return l != l ? -__builtin_inff() : fminf(l, 3.4028234663852886e38f) + 0.0f; }
-__device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
-// Integers in the order of numbers above -inf; -inf and NaN: none.
+// exp(x) = 2^t (1 + d), t = x / ln 2 in fp32 and d ln 2's share of what that rounding left out: the hardware's 2^t is good to its last bit, and so is this.  (Infinities and what is
+// beyond fp32 either way end at 200, whose exp is infinite or 0.)
+__device__ __forceinline__ float exp_of(float x) {
+  x = __builtin_amdgcn_fmed3f(x, -200.0f, 200.0f);
+  const float t = x * 1.4426950216293335f;                         // 1 / ln 2 = 1.44269502163 + 1.92596299e-8
+  const float d = fmaf(x, 1.925962991126617e-8f, fmaf(x, 1.4426950216293335f, -t));
+  const float p = __builtin_amdgcn_exp2f(t);
+  return t < 128.0f ? fmaf(p, d * 0.6931471805599453f, p) : p;
+}
+__device__ __forceinline__ float sigmoid(float l) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-l)); }   // (the reciprocal, too)
+// Integers in the order of numbers above -inf, and back; -inf and NaN: none.
 __device__ __forceinline__ int key_of(float v) {
   const int b = __float_as_int(v);
   return v > -__builtin_inff() ? b ^ ((b >> 31) & 0x7fffffff) : kNone;
 }
+__device__ __forceinline__ float value_of(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
 // Over the LPT lanes of a token, in each of them.
 struct IMax {
   __device__ __forceinline__ static int of(int a, int b) { return max(a, b); }
@@ -44,11 +54,12 @@ __device__ __forceinline__ int all_int(int v) {
   if (LPT == 16) return v;
   const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
   v = OP::of((int)a[0], (int)a[1]);
+  if (LPT == 32) return v;
   const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   return OP::of((int)b[0], (int)b[1]);
 }
 template <int LPT, class OP>
-__device__ __forceinline__ float all_float(float v) { return LPT == 16 ? row16_all<OP>(v) : wave_all<OP>(v); }
+__device__ __forceinline__ float all_float(float v) { return LPT == 16 ? row16_all<OP>(v) : LPT == 32 ? half_all<OP>(v) : wave_all<OP>(v); }
 
 // What a lane has of a token's logits: experts e0 .. e0 + V - 1, -inf beyond the last.
 template <int XT, int LPT, int V, bool SHORT>
@@ -57,14 +68,22 @@ struct Logits {
   int e0;
   __device__ __forceinline__ Logits(const RouteArgs& a, const void* row, int lane) {
     e0 = lane * V;
-    Run8<XT> r[V / 8];
+    if constexpr (V < 8) {
+      Run8<XT> r[V];
 #pragma unroll
-    for (int i = 0; i < V / 8; ++i) load_run<SHORT>(r[i], row, e0 + 8 * i, a.E);
+      for (int v = 0; v < V; ++v) r[v].load_part((const typename Run8<XT>::Elem*)row + min(e0 + v, a.E - 1), 1);
 #pragma unroll
-    for (int i = 0; i < V / 8; ++i) {
-      end_run<SHORT>(r[i], e0 + 8 * i, a.E);
+      for (int v = 0; v < V; ++v) l[v] = e0 + v < a.E ? as_logit(r[v].get(0)) : -__builtin_inff();
+    } else {
+      Run8<XT> r[V / 8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) l[8 * i + k] = e0 + 8 * i + k < a.E ? as_logit(r[i].get(k)) : -__builtin_inff();
+      for (int i = 0; i < V / 8; ++i) load_run<SHORT>(r[i], row, e0 + 8 * i, a.E);
+#pragma unroll
+      for (int i = 0; i < V / 8; ++i) {
+        end_run<SHORT>(r[i], e0 + 8 * i, a.E);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) l[8 * i + k] = e0 + 8 * i + k < a.E ? as_logit(r[i].get(k)) : -__builtin_inff();
+      }
     }
   }
   __device__ __forceinline__ float top() const {                   // the row's largest, 0 if there is none
@@ -97,46 +116,102 @@ __device__ __forceinline__ int scan_in_place(int* x, int n) {
   return all;
 }
 
-// LDS of a workgroup of `threads` threads.
-template <int LPT, bool GROUPS>
-size_t route_lds(const RouteArgs& a, int threads) {
-  return (size_t)a.E * 12 + kMaskTokens * a.k * 2 + 16 + (GROUPS ? (size_t)(threads / LPT) * (a.E + 2 * a.groups) * 4 : 0);
+// LDS: masks and running counts, the choices of 64 tokens with what they were chosen by, and for each token at work its scores (with a bias) and what its groups need.
+struct RouteLds {
+  int run, key, chosen, tokens, token_words;                       // byte offsets; words of a token
+  __host__ __device__ RouteLds(const RouteArgs& a, int lanes_experts, bool logits, bool groups) {
+    run = a.E * 8;
+    key = run + a.E * 4;
+    chosen = key + kMaskTokens * a.k * 4;
+    tokens = (chosen + kMaskTokens * a.k * 2 + 15) / 16 * 16;
+    token_words = (logits || !a.bias ? 0 : lanes_experts) + (groups ? lanes_experts + 2 * a.groups : 0);
+    token_words = (token_words + 3) / 4 * 4;
+  }
+};
+// Lanes of a token see each other's LDS: they are of one wave.
+__device__ __forceinline__ void token_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
-// Strikes out the experts of the groups that do not stay.  by: what the lane's experts' groups are judged by (-inf: masked).
+// The two largest of what lanes D apart have (first >= second).
+template <int D>
+__device__ __forceinline__ void join_two(float& first, float& second) {
+  float f, s;
+  if constexpr (D >= 16) {
+    const auto a = D == 16 ? __builtin_amdgcn_permlane16_swap(__float_as_int(first), __float_as_int(first), false, false)
+                           : __builtin_amdgcn_permlane32_swap(__float_as_int(first), __float_as_int(first), false, false);
+    const auto b = D == 16 ? __builtin_amdgcn_permlane16_swap(__float_as_int(second), __float_as_int(second), false, false)
+                           : __builtin_amdgcn_permlane32_swap(__float_as_int(second), __float_as_int(second), false, false);
+    first = __int_as_float(a[0]), f = __int_as_float(a[1]), second = __int_as_float(b[0]), s = __int_as_float(b[1]);
+  } else {
+    constexpr int CTRL = D == 1 ? kXor1 : D == 2 ? kXor2 : D == 4 ? kHalfMirror : kMirror;
+    f = __int_as_float(dpp<CTRL>(__float_as_int(first))), s = __int_as_float(dpp<CTRL>(__float_as_int(second)));
+  }
+  second = fmaxf(fminf(first, f), fmaxf(second, s));
+  first = fmaxf(first, f);
+}
+
+// Strikes out the experts of the groups that do not stay.  by: what the lane's experts' groups are judged by (-inf: masked).  Groups of 1, 2, 4, ... whole lanes are judged in
+// registers, others through LDS.
 template <int LPT, int V>
 __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, int e0, const float (&by)[V], int (&key)[V], float* mine) {
   const int per = a.E / a.groups;
-  float* score = mine + a.E;
-  int* keep = (int*)(score + a.groups);
-  auto wave_sync = [] {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  };
-  wave_sync();                                                     // (the token before has been read)
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-    if (e0 + v < a.E) mine[e0 + v] = by[v];
-  wave_sync();
   const float none = -__builtin_inff();
+  const int lanes = per / V;                                       // of a group
+  if (per == lanes * V && (lanes & (lanes - 1)) == 0) {
+    float first = none, second = none;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      second = fmaxf(second, fminf(first, by[v]));
+      first = fmaxf(first, by[v]);
+    }
+    if (lanes > 1) join_two<1>(first, second);
+    if (lanes > 2) join_two<2>(first, second);
+    if (lanes > 4) join_two<4>(first, second);
+    if (lanes > 8) join_two<8>(first, second);
+    if (LPT > 16 && lanes > 16) join_two<16>(first, second);
+    const float score = a.top2 && second > none ? first + second : first;
+    const int g = lane / lanes;
+    int better = 0;
+    for (int o = 0; o < a.groups; o += 4)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float s = __shfl(score, (o + i) * lanes, LPT);       // (beyond the last group: not counted)
+        better += o + i < a.groups && (s > score || (s == score && o + i < g));
+      }
+    if (better >= a.kept)
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = kNone;
+    return;
+  }
+  float* score = mine + LPT * V;
+  int* keep = (int*)(score + a.groups);
+  token_sync();                                                     // (the token before has been read)
+#pragma unroll
+  for (int v = 0; v < V; ++v) mine[e0 + v] = by[v];                // (room for all lanes' experts, those that are none too)
+  token_sync();
   for (int g = lane; g < a.groups; g += LPT) {
     float first = none, second = none;
-    for (int n = 0, i = g % per; n < per; ++n, i = i + 1 == per ? 0 : i + 1) {     // (started apart: neighbouring lanes on neighbouring banks)
+    int i = g % per;                                               // (started apart: neighbouring lanes on neighbouring banks)
+#pragma unroll 8
+    for (int n = 0; n < per; ++n, i = i + 1 == per ? 0 : i + 1) {
       const float c = mine[g * per + i];
       second = fmaxf(second, fminf(first, c));
       first = fmaxf(first, c);
     }
     score[g] = a.top2 && second > none ? first + second : first;
   }
-  wave_sync();
+  token_sync();
   for (int g = lane; g < a.groups; g += LPT) {
     const float s = score[g];
     int better = 0;
+#pragma unroll 8
     for (int o = 0; o < a.groups; ++o) better += score[o] > s || (score[o] == s && o < g);
     keep[g] = better < a.kept;
   }
-  wave_sync();
-  int g = e0 / per, left = (g + 1) * per - e0;
+  token_sync();
+  int g = min(e0, a.E - 1) / per, left = (g + 1) * per - e0;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     if (e0 + v < a.E && !keep[g]) key[v] = kNone;
@@ -144,38 +219,103 @@ __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, int e0
   }
 }
 
-// tokens: of a workgroup.  With the order: places inside the block to row_of and the block's counts to the workspace, or, alone, the whole order.
-template <int XT, int LPT, int V, bool GROUPS, bool SHORT>
-__global__ __launch_bounds__(GROUPS ? 512 : 1024) void route_kernel(RouteArgs a, int tokens, bool alone, int counts_pitch) {
+// A lane's experts by descending key, equal ones by index, as lists of up to eight: neighbours change places only where the right one is larger, which keeps
+// the order of equals.  place: four bits for each, where it came from.
+template <int V>
+struct Lists {
+  static constexpr int W = V < 8 ? V : 8, N = V / W;
+  int key[N][W];
+  uint32_t place[N];
+  __device__ __forceinline__ explicit Lists(const int (&k)[V]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      int at[W];
+#pragma unroll
+      for (int v = 0; v < W; ++v) at[v] = v, key[n][v] = k[n * W + v];
+#pragma unroll
+      for (int round = 0; round < W; ++round)
+#pragma unroll
+        for (int v = round & 1; v + 1 < W; v += 2) {
+          const int swap = key[n][v + 1] > key[n][v] ? at[v] ^ at[v + 1] : 0;     // (a choice between at[v] and at[v + 1] becomes one between all of them)
+          const int hi = max(key[n][v], key[n][v + 1]), lo = min(key[n][v], key[n][v + 1]);
+          key[n][v] = hi, key[n][v + 1] = lo, at[v] ^= swap, at[v + 1] ^= swap;
+        }
+      place[n] = 0;
+#pragma unroll
+      for (int v = 0; v < W; ++v) place[n] |= (uint32_t)at[v] << 4 * v;
+    }
+  }
+  __device__ __forceinline__ int first() const { return N == 1 ? key[0][0] : max(key[0][0], key[N - 1][0]); }
+  // which of the lane's experts the first one is (a key of the lane's largest), and the lists without it
+  __device__ __forceinline__ int index() const {
+    return N == 1 || key[0][0] >= key[N - 1][0] ? (int)(place[0] & 15) : W + (int)(place[N - 1] & 15);
+  }
+  __device__ __forceinline__ void drop(bool mine) {
+    const bool right = N > 1 && key[N - 1][0] > key[0][0];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const bool up = mine && right == (n > 0);
+#pragma unroll
+      for (int v = 0; v + 1 < W; ++v) key[n][v] = up ? key[n][v + 1] : key[n][v];
+      key[n][W - 1] = up ? kNone : key[n][W - 1];
+      place[n] = up ? place[n] >> 4 : place[n];
+    }
+  }
+};
+
+// Which lane of a token has the first of its experts with this property (64: none).
+template <int LPT>
+__device__ __forceinline__ int first_lane(bool mine) {
+  const uint64_t all = __ballot(mine);
+  if (LPT == 64) return all ? __builtin_ctzll(all) : 64;
+  const uint32_t half = threadIdx.x & 32 ? (uint32_t)(all >> 32) : (uint32_t)all;
+  if (LPT == 32) return half ? __builtin_ctz(half) : 64;
+  const uint32_t row = threadIdx.x & 16 ? half >> 16 : half & 0xffff;
+  return row ? __builtin_ctz(row) : 64;
+}
+
+// LOGITS: softmax without a bias, chosen by the logits themselves.  tokens: of a workgroup.  With the order: places inside the block to row_of and the block's counts to the
+// workspace, or, alone, the whole order.
+template <int XT, int LPT, int V, bool LOGITS, bool GROUPS, bool SHORT>
+__global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bool alone, int counts_pitch) {
+  fetch_arguments(a.logits, a.T, a.scale);
   extern __shared__ char mem[];
+  const RouteLds at(a, LPT * V, LOGITS, GROUPS);
   uint64_t* mask = (uint64_t*)mem;
-  int* run = (int*)(mask + a.E);                                   // the expert's pairs in the block's tokens before these
-  uint16_t* chosen = (uint16_t*)(run + a.E);
-  float* by_group = (float*)(((uintptr_t)(chosen + kMaskTokens * a.k) + 15) & ~(uintptr_t)15) + (GROUPS ? threadIdx.x / LPT * (a.E + 2 * a.groups) : 0);
+  int *run = (int*)(mem + at.run), *keys = (int*)(mem + at.key);   // run: the expert's pairs in the block's tokens before these
+  uint16_t* chosen = (uint16_t*)(mem + at.chosen);
+  float* own_scores = (float*)(mem + at.tokens) + threadIdx.x / LPT * at.token_words;
+  float* by_group = own_scores + (LOGITS || !a.bias ? 0 : LPT * V);
   const int tid = threadIdx.x, threads = blockDim.x, lane = tid % LPT;
   const int64_t b0 = (int64_t)blockIdx.x * tokens, b1 = b0 + tokens < a.T ? b0 + tokens : a.T;
   const bool order = a.row_of != nullptr;
+  const float none = -__builtin_inff();
   if (order)
     for (int e = tid; e < a.E; e += threads) run[e] = 0;
   for (int64_t s0 = b0; s0 < b1; s0 += kMaskTokens) {
     const int n = (int)(b1 - s0 < kMaskTokens ? b1 - s0 : kMaskTokens);
-    if (order) {
+    if (order)
       for (int e = tid; e < a.E; e += threads) mask[e] = 0;
-      __syncthreads();
-    }
     for (int i = tid / LPT; i < n; i += threads / LPT) {
       const int64_t t = s0 + i;
-      const void* row = elem_at(a.logits, t * a.ld, elem_bytes(XT));
-      const Logits<XT, LPT, V, SHORT> x(a, row, lane);
-      const float none = -__builtin_inff();
-      const float m = a.sigmoid ? 0.0f : x.top();
-      float total = 1.0f;
+      float bias[LOGITS ? 1 : V];
+      if (!LOGITS && a.bias) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) bias[v] = a.bias[min(lane * V + v, a.E - 1)];
+      } else if (!LOGITS) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) bias[v] = 0;
+      }
+      const Logits<XT, LPT, V, SHORT> x(a, elem_at(a.logits, t * a.ld, elem_bytes(XT)), lane);
+      // the row's largest, and the sum of exp behind it, where more than the chosen ones' own matter
+      float m = 0, total = 1.0f;
+      if (!a.sigmoid && (!LOGITS || !a.renorm || (GROUPS && a.top2))) m = x.top();
       int key[V];
-      if (!a.sigmoid && !a.bias) {                                 // by the logits themselves
+      if constexpr (LOGITS) {
         if (!a.renorm) {
           total = 0;
 #pragma unroll
-          for (int v = 0; v < V; ++v) total += expf(x.l[v] - m);
+          for (int v = 0; v < V; ++v) total += exp_of(x.l[v] - m);
           total = all_float<LPT, Add>(total);
         }
 #pragma unroll
@@ -183,7 +323,7 @@ __global__ __launch_bounds__(GROUPS ? 512 : 1024) void route_kernel(RouteArgs a,
         if (GROUPS) {
           float by[V];                                             // (scores up to a common factor)
 #pragma unroll
-          for (int v = 0; v < V; ++v) by[v] = key[v] == kNone ? none : a.top2 ? expf(x.l[v] - m) : x.l[v];
+          for (int v = 0; v < V; ++v) by[v] = key[v] == kNone ? none : a.top2 ? exp_of(x.l[v] - m) : x.l[v];
           keep_groups<LPT, V>(a, lane, x.e0, by, key, by_group);
         }
       } else {
@@ -192,66 +332,67 @@ __global__ __launch_bounds__(GROUPS ? 512 : 1024) void route_kernel(RouteArgs a,
 #pragma unroll
           for (int v = 0; v < V; ++v) s[v] = sigmoid(x.l[v]);
         } else {
-          total = 0;
+          float sum = 0;
 #pragma unroll
-          for (int v = 0; v < V; ++v) total += s[v] = expf(x.l[v] - m);
-          total = all_float<LPT, Add>(total);
-          const float inv = total > 0 ? 1.0f / total : 0.0f;
+          for (int v = 0; v < V; ++v) sum += s[v] = exp_of(x.l[v] - m);
+          sum = all_float<LPT, Add>(sum);
+          const float inv = sum > 0 ? 1.0f / sum : 0.0f;
 #pragma unroll
           for (int v = 0; v < V; ++v) s[v] *= inv;
         }
+        if (a.bias) {                                              // (the chosen ones' scores are read back there)
+          token_sync();                                            // (the token before has read its own)
+#pragma unroll
+          for (int v = 0; v < V; ++v) own_scores[x.e0 + v] = s[v];
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          if (a.bias && x.e0 + v < a.E) s[v] += a.bias[x.e0 + v];
+          s[v] += bias[v];
           s[v] = x.l[v] > none && s[v] > none ? s[v] + 0.0f : none;  // (NaN compares false)
           key[v] = key_of(s[v]);
         }
         if (GROUPS) keep_groups<LPT, V>(a, lane, x.e0, s, key, by_group);
       }
-      int id = -1;
+      // k times the largest of the lanes' first ones; of lanes that have it, the first; that lane notes the choice down
+      Lists<V> list(key);
       for (int j = 0; j < a.k; ++j) {
-        int best = key[0];
-#pragma unroll
-        for (int v = 1; v < V; ++v) best = max(best, key[v]);
-        best = all_int<LPT, IMax>(best);
-        int at = INT32_MAX;
-#pragma unroll
-        for (int v = V - 1; v >= 0; --v) at = key[v] == best ? x.e0 + v : at;
-        at = all_int<LPT, IMin>(at);
-#pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = x.e0 + v == at ? kNone : key[v];
-        if (lane == j && best != kNone) id = at;
+        const int first = list.first(), best = all_int<LPT, IMax>(first);
+        const bool mine = lane == first_lane<LPT>(first == best);
+        if (mine) {
+          chosen[i * a.k + j] = best == kNone ? 0xffff : (uint16_t)(x.e0 + list.index());
+          keys[i * a.k + j] = best;
+        }
+        list.drop(mine);
       }
-      // lane j: the weight of choice j
+      token_sync();
+      // lane j: choice j and its weight (without a bias the key says what it was chosen by)
+      const int id = lane < a.k ? (int)(int16_t)chosen[i * a.k + lane] : -1;
+      const int by = lane < a.k ? keys[i * a.k + lane] : kNone;
       float w = 0;
-      if (id >= 0) {
-        float l[1];
-        Run8<XT> one;
-        one.load_part((const typename Run8<XT>::Elem*)row + id, 1);
-        l[0] = as_logit(one.get(0));
-        w = a.sigmoid ? sigmoid(l[0]) : expf(l[0] - m);
-      }
+      if (LOGITS && a.renorm && !(GROUPS && a.top2)) m = value_of(all_int<LPT, IMax>(by));         // (no choice: not a number, and not used)
+      if (id >= 0) w = LOGITS ? exp_of(value_of(by) - m) : a.bias ? own_scores[id] : value_of(by);
       if (a.renorm) total = all_float<LPT, Add>(w);
       w = total > 0 ? a.scale * (w / total) : 0.0f;
       if (lane < a.k) {
         a.ids[t * a.k + lane] = id;
         a.weights[t * a.k + lane] = w;
-        if (order) {
-          chosen[i * a.k + lane] = (uint16_t)id;
-          if (id >= 0) atomicOr((unsigned long long*)&mask[id], 1ull << i);
-        }
       }
     }
     if (!order) continue;
-    __syncthreads();
+    lds_barrier();
+    for (int p = tid; p < n * a.k; p += threads) {
+      const uint16_t e = chosen[p];
+      if (e != 0xffff) atomicOr((unsigned long long*)&mask[e], 1ull << (p / a.k));
+    }
+    lds_barrier();
     if (alone) {                                                   // (one mask: run becomes where the expert's rows begin)
       for (int e = tid; e < a.E; e += threads) run[e] = __popcll(mask[e]);
-      __syncthreads();
+      lds_barrier();
       if (tid < 64) {
         const int all = scan_in_place(run, a.E);
         if (tid == 63) a.group_rows[a.E] = all;
       }
-      __syncthreads();
+      lds_barrier();
       for (int e = tid; e < a.E; e += threads) a.group_rows[e] = run[e];
     }
     for (int p = tid; p < n * a.k; p += threads) {
@@ -260,8 +401,8 @@ __global__ __launch_bounds__(GROUPS ? 512 : 1024) void route_kernel(RouteArgs a,
       a.row_of[s0 * a.k + p] = e == 0xffff ? -1 : run[e] + __popcll(mask[e] & ((1ull << i) - 1));
     }
     if (alone) return;
-    __syncthreads();
-    for (int e = tid; e < a.E; e += threads) run[e] += __popcll(mask[e]);
+    lds_barrier();
+    for (int e = tid; e < a.E; e += threads) run[e] += __popcll(mask[e]);   // (its own mask and count: the next tokens' mask may be cleared at once)
   }
   if (!order) return;
   uint16_t* counts = (uint16_t*)a.ws + (int64_t)blockIdx.x * counts_pitch;
@@ -271,9 +412,13 @@ __global__ __launch_bounds__(GROUPS ? 512 : 1024) void route_kernel(RouteArgs a,
 // Places inside the blocks to places of all.  counts: blocks x pitch, pitch a power of two from 8 on.
 __global__ __launch_bounds__(1024) void route_order_kernel(RouteArgs a, int tokens, int blocks, int pitch) {
   __shared__ int total[kRouteMaxE], before[kRouteMaxE];
+  fetch_arguments(a.logits, a.T, a.scale);
   const int tid = threadIdx.x, lane = tid & 63, runs = pitch / 8;
+  const int64_t p0 = (int64_t)blockIdx.x * tokens * a.k, end = a.T * a.k, p1 = p0 + (int64_t)tokens * a.k < end ? p0 + (int64_t)tokens * a.k : end;
+  int first_id = -1, first_row = 0;                                // (on their way while the counts are added up)
+  if (p0 + tid < p1) first_id = a.ids[p0 + tid], first_row = a.row_of[p0 + tid];
   for (int e = tid; e < pitch; e += 1024) total[e] = before[e] = 0;
-  __syncthreads();
+  lds_barrier();
   int all[8] = {}, upto[8] = {};
   const int c = tid & (runs - 1);                                  // a thread: eight experts of every (1024 / runs)-th block
 #pragma unroll 4
@@ -292,18 +437,17 @@ __global__ __launch_bounds__(1024) void route_order_kernel(RouteArgs a, int toke
   if (lane < runs)
 #pragma unroll
     for (int i = 0; i < 8; ++i) atomicAdd(&total[c * 8 + i], all[i]), atomicAdd(&before[c * 8 + i], upto[i]);   // (integers: any order, one sum)
-  __syncthreads();
+  lds_barrier();
   if (tid < 64) {
     const int n = scan_in_place(total, a.E);
     if (tid == 63 && blockIdx.x == 0) a.group_rows[a.E] = n;
   }
-  __syncthreads();
+  lds_barrier();
   if (blockIdx.x == 0)
     for (int e = tid; e < a.E; e += 1024) a.group_rows[e] = total[e];
-  const int64_t p0 = (int64_t)blockIdx.x * tokens * a.k, p1 = p0 + (int64_t)tokens * a.k, end = a.T * a.k;
-  for (int64_t p = p0 + tid; p < p1 && p < end; p += 1024) {
-    const int e = a.ids[p];
-    if (e >= 0) a.row_of[p] += total[e] + before[e];
+  for (int64_t p = p0 + tid; p < p1; p += 1024) {
+    const int e = p == p0 + tid ? first_id : a.ids[p];
+    if (e >= 0) a.row_of[p] = (p == p0 + tid ? first_row : a.row_of[p]) + total[e] + before[e];
   }
 }
 __global__ __launch_bounds__(1024) void route_no_tokens_kernel(int32_t* group_rows, int E) {
@@ -313,6 +457,7 @@ __global__ __launch_bounds__(1024) void route_no_tokens_kernel(int32_t* group_ro
 // Gradient of the logits; lanes as above.
 template <int XT, int LPT, int V, bool SHORT>
 __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a) {
+  fetch_arguments(a.logits, a.T, a.scale);
   const int lane = threadIdx.x % LPT;
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPT;
   if (t >= a.T) return;                                            // (all lanes of a token)
@@ -324,7 +469,7 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a) {
   const float m = a.sigmoid ? 0.0f : x.top();
   float s[V], total = 1.0f;
 #pragma unroll
-  for (int v = 0; v < V; ++v) s[v] = a.sigmoid ? sigmoid(x.l[v]) : expf(x.l[v] - m);
+  for (int v = 0; v < V; ++v) s[v] = a.sigmoid ? sigmoid(x.l[v]) : exp_of(x.l[v] - m);
   if (!a.sigmoid) {
     total = 0;
 #pragma unroll
@@ -336,7 +481,7 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a) {
     Run8<XT> one;
     one.load_part((const typename Run8<XT>::Elem*)row + id, 1);
     const float l = as_logit(one.get(0));
-    own = a.sigmoid ? sigmoid(l) : expf(l - m) * inv;
+    own = a.sigmoid ? sigmoid(l) : exp_of(l - m) * inv;
   }
   float along = 0;
   if (a.renorm) {                                                  // (then the sum of s ds is 0)
@@ -356,40 +501,49 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a) {
   }
   void* out = elem_at(a.dlogits, t * a.ld, elem_bytes(XT));
 #pragma unroll
-  for (int i = 0; i < V / 8; ++i) {
-    float d[8];
+  for (int i = 0; i < (V + 7) / 8; ++i) {
+    float d[8] = {};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 8 && k < V; ++k) {
       const int v = 8 * i + k;
       const float p = s[v] * inv;
       d[k] = x.l[v] == -__builtin_inff() ? 0.0f : a.sigmoid ? s[v] * (1.0f - s[v]) * ds[v] : p * (ds[v] - along);
     }
     Run8<XT> r;
     r.set(d);
-    store_run(r, out, x.e0 + 8 * i, a.E);
+    if (V < 8) {
+      if (x.e0 < a.E) r.store_part((typename Run8<XT>::Elem*)out + x.e0, min(V, a.E - x.e0));
+    } else {
+      store_run(r, out, x.e0 + 8 * i, a.E);
+    }
   }
 }
 
-// Lanes and experts a lane.
+// Lanes of a token and experts of a lane: as many lanes as the experts fill while the tokens do not fill the chip (`few`: that many tokens), else fewer, whose lists are longer.  us,
+// 4096 tokens of 128 experts, 64 lanes x 2 / 16 x 8: 6.0 / 5.2, their gradient 4.4 / 5.1; one token 3.8 / 4.2; 1000 tokens of 256 experts with groups, 64 x 4 / 32 x 8: 7.8 / 8.2.
 template <int LPT_, int V_, bool SHORT_ = false>
 struct RouteShape {
   static constexpr int LPT = LPT_, V = V_;
   static constexpr bool SHORT = SHORT_;
 };
 template <class F>
-void by_route_shape(int E, int k, F&& f) {
+void by_route_shape(bool few, int E, int k, F&& f) {
   if (E < 8) f(RouteShape<16, 8, true>());
-  else if (E <= 128 && k <= 16) f(RouteShape<16, 8>());
-  else if (E <= 256 && k <= 16) f(RouteShape<16, 16>());
+  else if (E <= 128 && (few || k > 16)) f(RouteShape<64, 2>());
+  else if (E <= 128) f(RouteShape<16, 8>());
+  else if (E <= 256 && (few || k > 32)) f(RouteShape<64, 4>());
+  else if (E <= 256) f(RouteShape<32, 8>());
   else if (E <= 512) f(RouteShape<64, 8>());
   else f(RouteShape<64, 16>());
 }
 
-// Blocks of tokens: 16 a block, more once that makes more than 256 of them; a block's counts have 16 bits.
+// Blocks of tokens: 8 a block, more once that makes more than 256 of them; a block's counts have 16 bits.  us, 1000 tokens in blocks of 4 / 8 / 16: 7.2 + 6.2 / 7.8 + 5.2 /
+// 9.7 + 5.0 for the two kernels, 4096 tokens in blocks of 16 / 32 / 64: 5.2 + 5.6 / 8.5 + 5.2 / 13.0 + 4.6 (before the lists were looked through as they are now).
 static int block_tokens(int64_t T) {
   if (T <= kMaskTokens) return kMaskTokens;
   const int64_t n = (T + 255) / 256;
-  return n <= 16 ? 16 : n <= 32 ? 32 : (int)std::min<int64_t>((n + kMaskTokens - 1) / kMaskTokens * kMaskTokens, 65536 - kMaskTokens);
+  if (n <= 32) return n <= 8 ? 8 : n <= 16 ? 16 : 32;
+  return (int)std::min<int64_t>((n + kMaskTokens - 1) / kMaskTokens * kMaskTokens, 65536 - kMaskTokens);
 }
 static int counts_pitch(int E) {
   int p = 8;
@@ -404,19 +558,24 @@ int64_t route_workspace_words(int64_t T, int E, int) {
 
 template <int XT>
 void launch_route_of(const RouteArgs& a, hipStream_t s) {
-  by_route_shape(a.E, a.k, [&](auto shape) {
+  by_route_shape(a.T <= 2048, a.E, a.k, [&](auto shape) {
     using S = decltype(shape);
     const int tokens = block_tokens(a.T), pitch = counts_pitch(a.E), blocks = (int)((a.T + tokens - 1) / tokens);
     const bool alone = blocks == 1;
-    const int here = (int)(a.T < tokens ? a.T : tokens);           // tokens at once: all of a mask's, as far as threads and LDS go
-    auto threads = [&](int most) { return std::min(most, (std::min(here, kMaskTokens) * S::LPT + 63) / 64 * 64); };
-    if (a.groups > 1) {
-      const int n = threads(512);
-      route_kernel<XT, S::LPT, S::V, true, S::SHORT><<<blocks, n, route_lds<S::LPT, true>(a, n), s>>>(a, tokens, alone, pitch);
-    } else {
-      const int n = threads(1024);
-      route_kernel<XT, S::LPT, S::V, false, S::SHORT><<<blocks, n, route_lds<S::LPT, false>(a, n), s>>>(a, tokens, alone, pitch);
-    }
+    const int here = (int)(a.T < tokens ? a.T : tokens);
+    auto launch = [&](auto logits, auto groups) {
+      constexpr bool L = decltype(logits)::value, G = decltype(groups)::value;
+      const RouteLds lds(a, S::LPT * S::V, L, G);
+      // tokens at once: all of a mask's, as far as threads and LDS go
+      int n = std::min(1024, (std::min(here, kMaskTokens) * S::LPT + 63) / 64 * 64);
+      while (n > 64 && lds.tokens + n / S::LPT * lds.token_words * 4 > 65536) n = (n / 2 + 63) / 64 * 64;
+      route_kernel<XT, S::LPT, S::V, L, G, S::SHORT><<<blocks, n, lds.tokens + n / S::LPT * lds.token_words * 4, s>>>(a, tokens, alone, pitch);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    const bool logits = !a.sigmoid && !a.bias;
+    if (a.groups > 1) logits ? launch(Yes(), Yes()) : launch(No(), Yes());
+    else logits ? launch(Yes(), No()) : launch(No(), No());
     if (a.row_of && !alone) route_order_kernel<<<blocks, 1024, 0, s>>>(a, tokens, blocks, pitch);
   });
 }
@@ -430,7 +589,7 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
 
 template <int XT>
 void launch_route_backward_of(const RouteArgs& all, hipStream_t s) {
-  by_route_shape(all.E, all.k, [&](auto shape) {
+  by_route_shape(all.T <= 8192, all.E, all.k, [&](auto shape) {
     using S = decltype(shape);
     constexpr int64_t kPiece = int64_t(1) << 24;                   // (a launch holds fewer than 2^32 threads)
     for (int64_t t0 = 0; t0 < all.T; t0 += kPiece) {

@@ -41,6 +41,7 @@ struct WaveAt {
 // Copies of elements of TYPE's size (fp32 as pairs of 16 bits).
 template <int TYPE, bool SHORT>
 __global__ __launch_bounds__(256) void rows_copy_kernel(RowsArgs a, int H, int64_t ldt, int64_t ldr) {
+  fetch_arguments(a.tokens, a.row_of, a.H);
   const WaveAt w(a.T, H);
   if (!w.there) return;
   constexpr int EB = elem_bytes(TYPE);
@@ -65,6 +66,7 @@ __global__ __launch_bounds__(256) void rows_copy_scales_kernel(RowsArgs a, int b
 
 template <int TYPE, bool SHORT>
 __global__ __launch_bounds__(256) void rows_quantise_kernel(RowsArgs a) {
+  fetch_arguments(a.tokens, a.row_of, a.H);
   const WaveAt w(a.T, a.H);
   if (!w.there) return;
   Run8<TYPE> v;
@@ -90,6 +92,7 @@ __global__ __launch_bounds__(256) void rows_quantise_kernel(RowsArgs a) {
 
 template <int TYPE, bool SHORT>
 __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
+  fetch_arguments(a.tokens, a.row_of, a.H);
   const WaveAt w(a.T, a.H);
   if (!w.there) return;
   constexpr int EB = elem_bytes(TYPE);
@@ -126,6 +129,7 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
 template <int TYPE, bool SHORT>
 __global__ __launch_bounds__(256) void rows_combine_backward_kernel(RowsArgs a) {
   constexpr int EB = elem_bytes(TYPE), RUNS = SHORT ? 1 : 4;
+  fetch_arguments(a.tokens, a.row_of, a.H);
   const int lane = threadIdx.x & 63;
   const int64_t pair = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (pair >= a.T * a.k) return;

@@ -9,6 +9,7 @@ namespace axe {
 constexpr int kBf16 = 1, kFp8 = 2, kF32 = 3, kF16 = 4;
 constexpr int elem_bytes(int type) { return type == kF32 ? 4 : type == kFp8 ? 1 : 2; }
 
+// (Every field of a line of 64 bytes comes with the others: the kernels name one of each, fetch_arguments.)
 struct NormArgs {
   const void *x, *r, *w;       // rows, residual (or null), weights (or null: ones); backward: dy, dsum, weights
   const void* h;               // backward: the normed rows

@@ -212,9 +212,27 @@ __device__ __forceinline__ void load_weights(float (&w)[RUNS][8], const void* p,
   else weights_of<SHORT, TPR, RUNS, kF16>(w, p, c, H);
 }
 
+// The arguments of a kernel lie in lines of 64 bytes that no cache holds yet, and the compiler fetches a field where it is used first: a kernel that comes to a line late waits
+// for memory once more.  One field of every line, named at the start, brings them all in together.
+template <class T>
+__device__ __forceinline__ void fetch_arguments(T of_a_line) { asm volatile("" ::"s"(of_a_line)); }
+template <class T, class... U>
+__device__ __forceinline__ void fetch_arguments(T first, U... others) {
+  fetch_arguments(first);
+  fetch_arguments(others...);
+}
+
+// A barrier of the workgroup that publishes what is in LDS, and nothing else: __syncthreads() also waits until the loads and stores of global memory under way are done, a
+// microsecond that no one here needs.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Exchanges inside a row of 16 lanes are operands of the instruction that uses them (DPP); between rows gfx950 swaps whole rows.
 template <int CTRL>
-__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false); }
+__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true); }
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
 struct Add {
   __device__ __forceinline__ static float of(float a, float b) { return a + b; }
@@ -222,7 +240,7 @@ struct Add {
 struct Max {
   __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); }
 };
-// v of all 16 lanes of a row, or of all 64, joined, in every lane.  (Each step joins lanes that hold the same number of values: the
+// v of all 16 lanes of a row, or of 32, or of all 64, joined, in every lane.  (Each step joins lanes that hold the same number of values: the
 // two sides of a step are the same in both lanes, so the results are the same bits.)
 template <class OP>
 __device__ __forceinline__ float row16_all(float v) {
@@ -232,10 +250,14 @@ __device__ __forceinline__ float row16_all(float v) {
   return OP::of(v, __int_as_float(dpp<kMirror>(__float_as_int(v))));
 }
 template <class OP>
-__device__ __forceinline__ float wave_all(float v) {
+__device__ __forceinline__ float half_all(float v) {               // 32 lanes
   v = row16_all<OP>(v);
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
-  v = OP::of(__int_as_float(a[0]), __int_as_float(a[1]));
+  return OP::of(__int_as_float(a[0]), __int_as_float(a[1]));
+}
+template <class OP>
+__device__ __forceinline__ float wave_all(float v) {
+  v = half_all<OP>(v);
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
   return OP::of(__int_as_float(b[0]), __int_as_float(b[1]));
 }
@@ -250,7 +272,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* lds, int wave) {
   if ((threadIdx.x & 63) == 0)
 #pragma unroll
     for (int i = 0; i < N; ++i) lds[i * WAVES + wave] = v[i];
-  __syncthreads();
+  lds_barrier();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     float t = 0;
