@@ -48,7 +48,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_kernel(NormArgs
 #pragma unroll
     for (int i = 0; i < RUNS; ++i) {
       x[i].set(h[i]);
-      store_run(x[i], rs, c + i * TPR * 8, a.H);
+      store_run<true>(x[i], rs, c + i * TPR * 8, a.H);             // (read again a layer later: past the caches)
     }
   }
   row_sums<1, WAVES>(sq, lds, threadIdx.x % TPR >> 6);
@@ -76,8 +76,8 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_kernel(NormArgs
 }
 
 // Gradients.  XT: h, dsum and dx; YT: dy.  A workgroup takes every gridDim-th row (rows of one wave: four at a time) and keeps its threads' columns of dw in
-// registers; what a workgroup has of dw goes to its row of the workspace, and a second kernel adds these rows up.
-template <int XT, int YT, int TPR, int RUNS, int ROWS, bool SHORT>
+// registers; what a workgroup has of dw goes to its row of the workspace, and a second kernel adds these rows up.  ONCE: loads past the caches.
+template <int XT, int YT, int TPR, int RUNS, int ROWS, bool ONCE, bool SHORT>
 __global__ __launch_bounds__(TPR * ROWS) void rmsnorm_backward_kernel(NormArgs a) {
   constexpr int WAVES = TPR / 64;
   __shared__ float lds[2][ROWS][2 * WAVES];
@@ -94,12 +94,12 @@ __global__ __launch_bounds__(TPR * ROWS) void rmsnorm_backward_kernel(NormArgs a
     const void *rd = elem_at(a.x, t * a.ldx, elem_bytes(YT)), *rh = elem_at(a.h, t * a.lds, elem_bytes(XT)), *rs = elem_at(a.r, t * a.ldr, elem_bytes(XT));
 #pragma unroll
     for (int i = 0; i < RUNS; ++i) {
-      load_run<SHORT>(dy[i], rd, c + i * TPR * 8, a.H);
-      load_run<SHORT>(h[i], rh, c + i * TPR * 8, a.H);
+      load_run<SHORT, ONCE>(dy[i], rd, c + i * TPR * 8, a.H);
+      load_run<SHORT, ONCE>(h[i], rh, c + i * TPR * 8, a.H);
     }
     if (a.r) {
 #pragma unroll
-      for (int i = 0; i < RUNS; ++i) load_run<SHORT>(ds[i], rs, c + i * TPR * 8, a.H);
+      for (int i = 0; i < RUNS; ++i) load_run<SHORT, ONCE>(ds[i], rs, c + i * TPR * 8, a.H);
     } else {
 #pragma unroll
       for (int i = 0; i < RUNS; ++i) ds[i].clear();
@@ -250,9 +250,12 @@ int64_t rmsnorm_workspace_words(int64_t T, int64_t H) {
 
 template <int XT, int YT>
 void launch_backward(const NormArgs& a, uint32_t groups, hipStream_t s) {
+  const bool once = a.T * a.H * (elem_bytes(YT) + elem_bytes(XT) * (a.r ? 3 : 2)) >= kReadsPastCaches;
   by_row_shape(a.H, [&](auto shape) {
     using S = decltype(shape);
-    rmsnorm_backward_kernel<XT, YT, S::TPR, S::RUNS, S::ROWS, S::SHORT><<<groups, S::TPR * S::ROWS, (S::ROWS - 1) * S::TPR * S::RUNS * 8 * 4, s>>>(a);
+    constexpr int lds = (S::ROWS - 1) * S::TPR * S::RUNS * 8 * 4;
+    if (once && !S::SHORT) rmsnorm_backward_kernel<XT, YT, S::TPR, S::RUNS, S::ROWS, !S::SHORT, S::SHORT><<<groups, S::TPR * S::ROWS, lds, s>>>(a);
+    else rmsnorm_backward_kernel<XT, YT, S::TPR, S::RUNS, S::ROWS, false, S::SHORT><<<groups, S::TPR * S::ROWS, lds, s>>>(a);
   });
 }
 

@@ -90,7 +90,8 @@ __global__ __launch_bounds__(256) void rows_quantise_kernel(RowsArgs a) {
   }
 }
 
-template <int TYPE, bool SHORT>
+// ROWS: rows whose loads are in flight together; ONCE: they go past the caches.
+template <int TYPE, int ROWS, bool ONCE, bool SHORT>
 __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
   fetch_arguments(a.tokens, a.row_of, a.H);
   const WaveAt w(a.T, a.H);
@@ -104,19 +105,19 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
   if (a.add) load_run<SHORT>(v, elem_at(a.add, w.t * a.ldt, EB), w.c, a.H), end_run<SHORT>(v, w.c, a.H);
 #pragma unroll
   for (int k = 0; k < 8; ++k) sum[k] = v.get(k);
-  for (int j0 = 0; j0 < a.k; j0 += 8) {
-    Run8<TYPE> c[8];
-    int r[8];
+  for (int j0 = 0; j0 < a.k; j0 += ROWS) {
+    Run8<TYPE> c[ROWS];
+    int r[ROWS];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < ROWS; ++j) {                               // (a row that is none: the first one, whose bits are then dropped -- a branch would put each load behind the one before)
       r[j] = j0 + j < a.k ? rows.row(j0 + j) : -1;
-      if (r[j] >= 0) load_run<SHORT>(c[j], elem_at(a.rows, r[j] * a.ldr, EB), w.c, a.H);
+      load_run<SHORT, ONCE>(c[j], elem_at(a.rows, max(r[j], 0) * a.ldr, EB), w.c, a.H);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (r[j] < 0) continue;
+    for (int j = 0; j < ROWS; ++j) {
+      c[j].keep(r[j] >= 0);
       end_run<SHORT>(c[j], w.c, a.H);
-      const float wj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight), j0 + j));
+      const float wj = r[j] >= 0 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight), (j0 + j) & 63)) : 0.0f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) sum[k] += wj * c[j].get(k);
     }
@@ -125,11 +126,11 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
   store_run(v, elem_at(a.to_tokens, w.t * a.ldt, EB), w.c, a.H);
 }
 
-// A wave per pair.
-template <int TYPE, bool SHORT>
+// A wave per pair, RUNS runs of a lane at a time.  DOT: the rows are read, for dweights.  PAST: what goes past the caches, 1: stores, 2: loads of the rows, too.
+template <int TYPE, int RUNS, bool DOT, int PAST, bool SHORT>
 __global__ __launch_bounds__(256) void rows_combine_backward_kernel(RowsArgs a) {
-  constexpr int EB = elem_bytes(TYPE), RUNS = SHORT ? 1 : 4;
   fetch_arguments(a.tokens, a.row_of, a.H);
+  constexpr int EB = elem_bytes(TYPE);
   const int lane = threadIdx.x & 63;
   const int64_t pair = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (pair >= a.T * a.k) return;
@@ -140,36 +141,36 @@ __global__ __launch_bounds__(256) void rows_combine_backward_kernel(RowsArgs a) 
     const float w = a.weights ? a.weights[pair] : 1.0f;
     const void *rd = elem_at(a.tokens, t * a.ldt, EB), *rc = elem_at(a.rows, r * a.ldr, EB);
     void* ro = elem_at(a.to_rows, r * a.ldr, EB);
-    for (int c0 = 0; c0 < a.H; c0 += kSlab * RUNS) {
+    for (int c0 = lane * 8; c0 - lane * 8 < a.H; c0 += kSlab * RUNS) {
       Run8<TYPE> d[RUNS], c[RUNS];
 #pragma unroll
-      for (int i = 0; i < RUNS; ++i) {
-        if (c0 + i * kSlab >= a.H) break;
-        load_run<SHORT>(d[i], rd, c0 + i * kSlab + lane * 8, a.H);
-        if (a.rows) load_run<SHORT>(c[i], rc, c0 + i * kSlab + lane * 8, a.H);
+      for (int i = 0; i < RUNS; ++i) {                             // (runs behind the row's end: its last one, and zeros in the end)
+        if (DOT) load_run<SHORT, PAST == 2>(c[i], rc, c0 + i * kSlab, a.H);
+        load_run<SHORT>(d[i], rd, c0 + i * kSlab, a.H);
       }
 #pragma unroll
       for (int i = 0; i < RUNS; ++i) {
-        const int ci = c0 + i * kSlab + lane * 8;
-        if (c0 + i * kSlab >= a.H) break;
-        end_run<SHORT>(d[i], ci, a.H);
-        if (a.rows) {
-          end_run<SHORT>(c[i], ci, a.H);
+        end_run<SHORT>(d[i], c0 + i * kSlab, a.H);
+        if (DOT) {
+          end_run<SHORT>(c[i], c0 + i * kSlab, a.H);
 #pragma unroll
           for (int k = 0; k < 8; ++k) dot += d[i].get(k) * c[i].get(k);
         }
-        if (a.to_rows) {
+      }
+      if (a.to_rows) {
+#pragma unroll
+        for (int i = 0; i < RUNS; ++i) {
           float v[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) v[k] = w * d[i].get(k);
           d[i].set(v);
-          store_run(d[i], ro, ci, a.H);
+          store_run<PAST != 0>(d[i], ro, c0 + i * kSlab, a.H);
         }
       }
     }
-    dot = wave_sum(dot);
+    if (DOT) dot = wave_sum(dot);
   }
-  if (a.dweights && lane == 0) a.dweights[pair] = dot;
+  if (DOT && lane == 0) a.dweights[pair] = dot;
 }
 
 // A launch holds fewer than 2^32 threads: calls of more waves go in pieces of whole tokens.
@@ -227,26 +228,46 @@ hipError_t launch_rows_dispatch(const RowsArgs& a, hipStream_t s) {
   });
 }
 
-template <int TYPE>
+// What a call of all its pairs moves.
+static int64_t rows_bytes(const RowsArgs& a, int rows_times, int tokens_times) { return ((int64_t)a.k * rows_times + tokens_times) * a.T * a.H * elem_bytes(a.r_type); }
+
+template <int TYPE, bool ONCE>
 hipError_t launch_combine(const RowsArgs& a, hipStream_t s) {
   return in_pieces(a, slabs_of(a.H), [&](const RowsArgs& p, uint32_t groups) {
-    if (a.H < 8) rows_combine_kernel<TYPE, true><<<groups, 256, 0, s>>>(p);
-    else rows_combine_kernel<TYPE, false><<<groups, 256, 0, s>>>(p);
+    if (a.H < 8) rows_combine_kernel<TYPE, 8, false, true><<<groups, 256, 0, s>>>(p);
+    else if (a.k == 1) rows_combine_kernel<TYPE, 1, ONCE, false><<<groups, 256, 0, s>>>(p);
+    else if (a.k == 2) rows_combine_kernel<TYPE, 2, ONCE, false><<<groups, 256, 0, s>>>(p);
+    else if (a.k <= 4) rows_combine_kernel<TYPE, 4, ONCE, false><<<groups, 256, 0, s>>>(p);
+    else rows_combine_kernel<TYPE, 8, ONCE, false><<<groups, 256, 0, s>>>(p);
   });
+}
+template <bool ONCE>
+hipError_t launch_combine_of(const RowsArgs& a, hipStream_t s) {
+  return a.r_type == kBf16 ? launch_combine<kBf16, ONCE>(a, s) : a.r_type == kF16 ? launch_combine<kF16, ONCE>(a, s) : launch_combine<kF32, ONCE>(a, s);
 }
 hipError_t launch_rows_combine(const RowsArgs& a, hipStream_t s) {
-  return a.r_type == kBf16 ? launch_combine<kBf16>(a, s) : a.r_type == kF16 ? launch_combine<kF16>(a, s) : launch_combine<kF32>(a, s);
+  return rows_bytes(a, 1, a.add ? 2 : 1) >= kPastCaches ? launch_combine_of<true>(a, s) : launch_combine_of<false>(a, s);
 }
 
-template <int TYPE>
+template <int TYPE, bool DOT, int PAST>
 hipError_t launch_combine_backward(const RowsArgs& a, hipStream_t s) {
   return in_pieces(a, a.k, [&](const RowsArgs& p, uint32_t groups) {
-    if (a.H < 8) rows_combine_backward_kernel<TYPE, true><<<groups, 256, 0, s>>>(p);
-    else rows_combine_backward_kernel<TYPE, false><<<groups, 256, 0, s>>>(p);
+    if (a.H < 8) rows_combine_backward_kernel<TYPE, 1, DOT, 0, true><<<groups, 256, 0, s>>>(p);
+    else if (a.H <= kSlab) rows_combine_backward_kernel<TYPE, 1, DOT, PAST, false><<<groups, 256, 0, s>>>(p);
+    else if (a.H <= 2 * kSlab) rows_combine_backward_kernel<TYPE, 2, DOT, PAST, false><<<groups, 256, 0, s>>>(p);
+    else rows_combine_backward_kernel<TYPE, 4, DOT, PAST, false><<<groups, 256, 0, s>>>(p);
   });
 }
+template <bool DOT, int PAST>
+hipError_t launch_combine_backward_of(const RowsArgs& a, hipStream_t s) {
+  return a.r_type == kBf16 ? launch_combine_backward<kBf16, DOT, PAST>(a, s)
+                           : a.r_type == kF16 ? launch_combine_backward<kF16, DOT, PAST>(a, s) : launch_combine_backward<kF32, DOT, PAST>(a, s);
+}
 hipError_t launch_rows_combine_backward(const RowsArgs& a, hipStream_t s) {
-  return a.r_type == kBf16 ? launch_combine_backward<kBf16>(a, s) : a.r_type == kF16 ? launch_combine_backward<kF16>(a, s) : launch_combine_backward<kF32>(a, s);
+  const int64_t bytes = rows_bytes(a, (a.dweights ? 1 : 0) + (a.to_rows ? 1 : 0), 1);
+  if (!a.dweights) return bytes >= kPastCaches ? launch_combine_backward_of<false, 1>(a, s) : launch_combine_backward_of<false, 0>(a, s);
+  return bytes >= kAllPastCaches ? launch_combine_backward_of<true, 2>(a, s)
+                                 : bytes >= kPastCaches ? launch_combine_backward_of<true, 1>(a, s) : launch_combine_backward_of<true, 0>(a, s);
 }
 
 }  // namespace axe

@@ -44,6 +44,13 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s);
 hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s);
 int64_t route_workspace_words(int64_t T, int E, int k);
 
+// Bytes of a call from which its large operands go past the caches (non-temporal): they do not stay until they are touched again, and evicting for them costs time.  us, three sets of
+// buffers in turn.  Loads of combine's rows, cached / past: 2048 tokens of 8 rows of 2048 bf16 (72 MiB in all) 12.8 / 14.4, 3000 (105 MiB) 22.8 / 19.8, 4096 30.9 / 27.1.
+// Its gradient's stores: 1024 (68 MiB) 12.8 / 12.8, 1500 (100 MiB) 20.6 / 17.6, 2048 30.4 / 23.4; its loads as well: 2048 (136 MiB) 23.4 / 27.7, 4096 (272 MiB) 56.2 / 52.4.  The norm's gradient's loads:
+// 4096 x 2048 (64 MiB) 13.4 / 15.8, 3000 x 8192 (188 MiB) 42.4 / 39.2, 4096 x 8192 55.9 / 53.0.  dispatch keeps its stores in the caches: past them 4096 tokens to e4m3 take
+// 14.7 for 15.4, but with the next kernel, which reads them, 45.4 for 41.4.
+constexpr int64_t kPastCaches = int64_t(96) << 20, kReadsPastCaches = int64_t(128) << 20, kAllPastCaches = int64_t(256) << 20;
+
 struct RowsArgs {
   const void *tokens, *rows;   // what is read of the two matrices
   void *to_tokens, *to_rows;   // what is written

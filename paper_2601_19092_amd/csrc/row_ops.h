@@ -15,13 +15,21 @@ namespace axe {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <class V>
-struct __attribute__((packed, aligned(1))) Anywhere {
-  V v;
+struct AnywhereOf {
+  typedef V T __attribute__((aligned(1)));
 };
-template <class V>
-__device__ __forceinline__ V load_bits(const void* p) { return ((const Anywhere<V>*)p)->v; }
-template <class V>
-__device__ __forceinline__ void store_bits(void* p, V v) { ((Anywhere<V>*)p)->v = v; }
+// NT: data that this kernel touches once and leaves to the last-level cache's other tenants (see where it is asked for).
+template <class V, bool NT = false>
+__device__ __forceinline__ V load_bits(const void* p) {
+  using A = typename AnywhereOf<V>::T;
+  return NT ? __builtin_nontemporal_load((const A*)p) : *(const A*)p;
+}
+template <bool NT = false, class V>
+__device__ __forceinline__ void store_bits(void* p, V v) {
+  using A = typename AnywhereOf<V>::T;
+  if (NT) __builtin_nontemporal_store(v, (A*)p);
+  else *(A*)p = v;
+}
 
 template <int TYPE>
 struct Run8;
@@ -30,8 +38,11 @@ struct Run8<kBf16> {
   using Elem = uint16_t;
   u32x4 b;
   __device__ __forceinline__ void clear() { b = u32x4{}; }
-  __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x4>(p); }
-  __device__ __forceinline__ void store(void* p) const { store_bits(p, b); }
+  __device__ __forceinline__ void keep(bool on) { b = on ? b : u32x4{}; }
+  template <bool NT>
+  __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x4, NT>(p); }
+  template <bool NT>
+  __device__ __forceinline__ void store(void* p) const { store_bits<NT>(p, b); }
   __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? b[i >> 1] & 0xffff0000u : b[i >> 1] << 16); }
   __device__ __forceinline__ void set(const float (&v)[8]) {
 #pragma unroll
@@ -70,8 +81,11 @@ struct Run8<kF16> {
   using Elem = uint16_t;
   u32x4 b;
   __device__ __forceinline__ void clear() { b = u32x4{}; }
-  __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x4>(p); }
-  __device__ __forceinline__ void store(void* p) const { store_bits(p, b); }
+  __device__ __forceinline__ void keep(bool on) { b = on ? b : u32x4{}; }
+  template <bool NT>
+  __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x4, NT>(p); }
+  template <bool NT>
+  __device__ __forceinline__ void store(void* p) const { store_bits<NT>(p, b); }
   __device__ __forceinline__ float get(int i) const { return (float)__builtin_bit_cast(_Float16, (uint16_t)(b[i >> 1] >> (i & 1) * 16)); }
   __device__ __forceinline__ void set(const float (&v)[8]) {
 #pragma unroll
@@ -110,8 +124,11 @@ struct Run8<kF32> {
   using Elem = uint32_t;
   u32x4 b[2];
   __device__ __forceinline__ void clear() { b[0] = b[1] = u32x4{}; }
-  __device__ __forceinline__ void load(const void* p) { b[0] = load_bits<u32x4>(p), b[1] = load_bits<u32x4>((const char*)p + 16); }
-  __device__ __forceinline__ void store(void* p) const { store_bits(p, b[0]), store_bits((char*)p + 16, b[1]); }
+  __device__ __forceinline__ void keep(bool on) { b[0] = on ? b[0] : u32x4{}, b[1] = on ? b[1] : u32x4{}; }
+  template <bool NT>
+  __device__ __forceinline__ void load(const void* p) { b[0] = load_bits<u32x4, NT>(p), b[1] = load_bits<u32x4, NT>((const char*)p + 16); }
+  template <bool NT>
+  __device__ __forceinline__ void store(void* p) const { store_bits<NT>(p, b[0]), store_bits<NT>((char*)p + 16, b[1]); }
   __device__ __forceinline__ float get(int i) const { return __uint_as_float(b[i >> 2][i & 3]); }
   __device__ __forceinline__ void set(const float (&v)[8]) {
 #pragma unroll
@@ -145,8 +162,10 @@ struct Run8<kFp8> {
   using Elem = uint8_t;
   u32x2 b;
   __device__ __forceinline__ void clear() { b = u32x2{}; }
-  __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x2>(p); }
-  __device__ __forceinline__ void store(void* p) const { store_bits(p, b); }
+  template <bool NT>
+  __device__ __forceinline__ void load(const void* p) { b = load_bits<u32x2, NT>(p); }
+  template <bool NT>
+  __device__ __forceinline__ void store(void* p) const { store_bits<NT>(p, b); }
   __device__ __forceinline__ void set(const float (&v)[8]);
   __device__ __forceinline__ void down(int n) {
     const uint64_t v = n < 8 ? ((uint64_t)b[1] << 32 | b[0]) >> n * 8 : 0;
@@ -168,20 +187,20 @@ struct Run8<kFp8> {
 // The run at element i of a row of H elements, in two steps; what lies past the row's end comes out as zero.  A run that would reach past the end (or lies behind
 // it) is read as the row's last eight elements and moved down in the second step: the loads of all threads are then single instructions with no branch
 // around them, and all of a thread's can be in flight.  Rows of fewer than eight elements (SHORT) are put together from what they have.
-template <bool SHORT, int TYPE>
+template <bool SHORT, bool NT = false, int TYPE>
 __device__ __forceinline__ void load_run(Run8<TYPE>& r, const void* row, int i, int H) {
   using E = typename Run8<TYPE>::Elem;
   if (SHORT) r.load_part((const E*)row, i == 0 ? H : 0);
-  else r.load((const E*)row + (i + 8 <= H ? i : H - 8));
+  else r.template load<NT>((const E*)row + (i + 8 <= H ? i : H - 8));
 }
 template <bool SHORT, int TYPE>
 __device__ __forceinline__ void end_run(Run8<TYPE>& r, int i, int H) {
   if (!SHORT && i + 8 > H) r.down(i < H ? i + 8 - H : 8);
 }
-template <int TYPE>
+template <bool NT = false, int TYPE>
 __device__ __forceinline__ void store_run(const Run8<TYPE>& r, void* row, int i, int H) {
   using E = typename Run8<TYPE>::Elem;
-  if (i + 8 <= H) r.store((E*)row + i);
+  if (i + 8 <= H) r.template store<NT>((E*)row + i);
   else if (i < H) r.store_part((E*)row + i, H - i);
 }
 template <class E>
