@@ -161,7 +161,7 @@ __global__ __launch_bounds__(TPR * ROWS) void rmsnorm_backward_kernel(NormArgs a
 }
 
 // dw: the sum of n rows of the workspace, 64 columns a workgroup: wave i adds the rows i, i + 16, ... -- loads without an order, eight in flight -- and the sums of the
-// sixteen waves are joined through LDS.
+// sixteen waves are joined through LDS.  us, 512 rows of 2048 / 8192: 3.8 / 4.9; 16 columns a workgroup 3.9 / 7.0.
 __global__ __launch_bounds__(1024) void rmsnorm_dweight_kernel(const float* ws, float* dw, int n, int H) {
   __shared__ float lds[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, at = c < H ? c : H - 1;
