@@ -154,6 +154,7 @@ RouteArgs route_args(const axe_route_desc_t* g, const Mat& m, const void* logits
   // all groups kept: they decide nothing
   a.groups = g->groups_kept == g->groups ? 1 : g->groups, a.kept = a.groups == 1 ? 1 : g->groups_kept;
   a.top2 = g->group_score == AXE_ROUTE_GROUP_TOP2;
+  a.per = g->E / a.groups;
   a.scale = g->scale;
   return a;
 }

@@ -95,19 +95,41 @@ struct Logits {
   }
 };
 
+// Sums over lanes. The shifts are operands of the additions (DPP): within a row of 16 lanes, then from the last lane of a row to the next one, of the first two rows to the others.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int plus_from(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int sums_up_to(int v) {                 // of this lane and those before it
+  v = plus_from<0x111, 0xf>(v);                                    // row_shr 1, 2, 4, 8
+  v = plus_from<0x112, 0xf>(v);
+  v = plus_from<0x114, 0xf>(v);
+  v = plus_from<0x118, 0xf>(v);
+  v = plus_from<0x142, 0xa>(v);                                    // row_bcast 15 to rows 1 and 3
+  return plus_from<0x143, 0xc>(v);                                 // row_bcast 31 to rows 2 and 3
+}
+// of the lanes that are the same mod N (1, 2, 4, ...), in each of them
+template <int N>
+__device__ __forceinline__ int sums_mod(int v) {
+  if (N <= 1) v += dpp<0x121>(v);                                  // row_ror 1, 2, 4, 8
+  if (N <= 2) v += dpp<0x122>(v);
+  if (N <= 4) v += dpp<0x124>(v);
+  if (N <= 8) v += dpp<0x128>(v);
+  if (N <= 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = (int)a[0] + (int)a[1];
+  }
+  if (N <= 32) {
+    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = (int)a[0] + (int)a[1];
+  }
+  return v;
+}
 // Exclusive sums of n <= 1024 numbers in LDS, by one wave; the last lane's return value is the sum of all.
 __device__ __forceinline__ int scan_in_place(int* x, int n) {
   const int lane = threadIdx.x & 63, per = (n + 63) / 64, first = lane * per;
   int s = 0;
   for (int i = first; i < first + per && i < n; ++i) s += x[i];
-  int before = s;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(before, d);
-    if (lane >= d) before += o;
-  }
-  const int all = before;
-  before -= s;
+  const int all = sums_up_to(s);
+  int before = all - s;
   for (int i = first; i < first + per && i < n; ++i) {
     const int c = x[i];
     x[i] = before;
@@ -156,9 +178,9 @@ __device__ __forceinline__ void join_two(float& first, float& second) {
 // registers, others through LDS.
 template <int LPT, int V>
 __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, int e0, const float (&by)[V], int (&key)[V], float* mine) {
-  const int per = a.E / a.groups;
+  const int per = a.per;
   const float none = -__builtin_inff();
-  const int lanes = per / V;                                       // of a group
+  const int lanes = per / V;                                       // of a group (V is a power of two)
   if (per == lanes * V && (lanes & (lanes - 1)) == 0) {
     float first = none, second = none;
 #pragma unroll
@@ -172,12 +194,13 @@ __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, int e0
     if (lanes > 8) join_two<8>(first, second);
     if (LPT > 16 && lanes > 16) join_two<16>(first, second);
     const float score = a.top2 && second > none ? first + second : first;
-    const int g = lane / lanes;
+    const int g = lane >> (31 - __builtin_clz(lanes));
     int better = 0;
     for (int o = 0; o < a.groups; o += 4)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float s = __shfl(score, (o + i) * lanes, LPT);       // (beyond the last group: not counted)
+        // (beyond the last group: not counted)
+        const float s = LPT == 64 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(score), (o + i) * lanes & 63)) : __shfl(score, (o + i) * lanes, LPT);
         better += o + i < a.groups && (s > score || (s == score && o + i < g));
       }
     if (better >= a.kept)
@@ -409,20 +432,22 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
   for (int e = tid; e < counts_pitch; e += threads) counts[e] = e < a.E ? (uint16_t)run[e] : 0;
 }
 
-// Places inside the blocks to places of all.  counts: blocks x pitch, pitch a power of two from 8 on.
-__global__ __launch_bounds__(1024) void route_order_kernel(RouteArgs a, int tokens, int blocks, int pitch) {
-  __shared__ int total[kRouteMaxE], before[kRouteMaxE];
+// Places inside the blocks to places of all.  The workspace: for each block the counts of RUNS runs of eight experts.
+template <int RUNS>
+__global__ __launch_bounds__(1024) void route_order_kernel(RouteArgs a, int tokens, int blocks) {
+  constexpr int pitch = 8 * RUNS;
+  __shared__ int sum[2][pitch], total[pitch], before[pitch];
   fetch_arguments(a.logits, a.T, a.scale);
-  const int tid = threadIdx.x, lane = tid & 63, runs = pitch / 8;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int64_t p0 = (int64_t)blockIdx.x * tokens * a.k, end = a.T * a.k, p1 = p0 + (int64_t)tokens * a.k < end ? p0 + (int64_t)tokens * a.k : end;
   int first_id = -1, first_row = 0;                                // (on their way while the counts are added up)
   if (p0 + tid < p1) first_id = a.ids[p0 + tid], first_row = a.row_of[p0 + tid];
-  for (int e = tid; e < pitch; e += 1024) total[e] = before[e] = 0;
+  for (int e = tid; e < pitch; e += 1024) sum[0][e] = sum[1][e] = 0;
   lds_barrier();
   int all[8] = {}, upto[8] = {};
-  const int c = tid & (runs - 1);                                  // a thread: eight experts of every (1024 / runs)-th block
+  const int c = tid & (RUNS - 1);                                  // a thread: eight experts of every (1024 / RUNS)-th block
 #pragma unroll 4
-  for (int b = tid / runs; b < blocks; b += 1024 / runs) {
+  for (int b = tid / RUNS; b < blocks; b += 1024 / RUNS) {
     const u32x4 v = load_bits<u32x4>((const uint16_t*)a.ws + (int64_t)b * pitch + c * 8);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -431,12 +456,13 @@ __global__ __launch_bounds__(1024) void route_order_kernel(RouteArgs a, int toke
       if (b < (int)blockIdx.x) upto[2 * i] += lo, upto[2 * i + 1] += hi;
     }
   }
-  for (int d = runs; d < 64; d <<= 1)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) all[i] += __shfl_xor(all[i], d), upto[i] += __shfl_xor(upto[i], d);
-  if (lane < runs)
+  for (int i = 0; i < 8; ++i) all[i] = sums_mod<RUNS>(all[i]), upto[i] = sums_mod<RUNS>(upto[i]);
+  if (lane < RUNS)                                                 // (integers: any order, one sum; lanes side by side in LDS: expert 8 c + i at i * RUNS + c)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) atomicAdd(&total[c * 8 + i], all[i]), atomicAdd(&before[c * 8 + i], upto[i]);   // (integers: any order, one sum)
+    for (int i = 0; i < 8; ++i) atomicAdd(&sum[0][i * RUNS + c], all[i]), atomicAdd(&sum[1][i * RUNS + c], upto[i]);
+  lds_barrier();
+  for (int e = tid; e < pitch; e += 1024) total[e] = sum[0][(e & 7) * RUNS + (e >> 3)], before[e] = sum[1][(e & 7) * RUNS + (e >> 3)];
   lds_barrier();
   if (tid < 64) {
     const int n = scan_in_place(total, a.E);
@@ -557,6 +583,12 @@ int64_t route_workspace_words(int64_t T, int E, int) {
   return (T + tokens - 1) / tokens * counts_pitch(E) / 2;
 }
 
+template <int RUNS>
+void launch_order(const RouteArgs& a, int tokens, int blocks, int pitch, hipStream_t s) {
+  if (pitch == 8 * RUNS) route_order_kernel<RUNS><<<blocks, 1024, 0, s>>>(a, tokens, blocks);
+  else if constexpr (8 * RUNS < kRouteMaxE) launch_order<2 * RUNS>(a, tokens, blocks, pitch, s);
+}
+
 template <int XT>
 void launch_route_of(const RouteArgs& a, hipStream_t s) {
   by_route_shape(a.T <= 2048, a.E, a.k, [&](auto shape) {
@@ -577,7 +609,7 @@ void launch_route_of(const RouteArgs& a, hipStream_t s) {
     const bool logits = !a.sigmoid && !a.bias;
     if (a.groups > 1) logits ? launch(Yes(), Yes()) : launch(No(), Yes());
     else logits ? launch(Yes(), No()) : launch(No(), No());
-    if (a.row_of && !alone) route_order_kernel<<<blocks, 1024, 0, s>>>(a, tokens, blocks, pitch);
+    if (a.row_of && !alone) launch_order<1>(a, tokens, blocks, pitch, s);
   });
 }
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {

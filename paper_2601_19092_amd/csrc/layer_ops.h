@@ -37,6 +37,7 @@ struct RouteArgs {
   void* dlogits;
   int64_t T, ld;
   int32_t E, k, type, sigmoid, renorm, groups, kept, top2;
+  int32_t per;                 // experts of a group
   float scale;
 };
 constexpr int kRouteMaxE = 1024, kRouteMaxK = 64, kRouteMaxGroups = 64;
