@@ -400,7 +400,7 @@ def test_route_of_no_tokens_and_without_the_order():
     assert torch.equal(with_order[0], without[0]) and torch.equal(with_order[1], without[1])
 
 
-@pytest.mark.parametrize("T,E,k", [(63, 128, 8), (64, 128, 8), (66, 128, 8), (257, 8, 2), (1024, 1024, 8), (4096, 128, 8), (4097, 60, 4), (33333, 256, 8), (20000, 8, 1), (9000, 1000, 64)])
+@pytest.mark.parametrize("T,E,k", [(16, 128, 8), (17, 128, 8), (63, 128, 8), (64, 128, 8), (65, 128, 8), (66, 128, 8), (48, 256, 8), (49, 256, 8), (64, 256, 8), (32, 512, 20), (33, 512, 20), (2048, 200, 8), (2049, 200, 8), (257, 8, 2), (1024, 1024, 8), (4096, 128, 8), (4097, 60, 4), (33333, 256, 8), (20000, 8, 1), (9000, 1000, 64)])
 def test_experts_order_of_many_tokens(T, E, k):
     g = torch.Generator(device="cuda").manual_seed(T)
     logits = torch.randn((T, E), generator=g, device="cuda").to(torch.bfloat16).float()
