@@ -9,6 +9,9 @@
  *   axe_gemm          layout-driven tiled dense GEMM, bf16 / block-scaled fp8 (Sec. 3.2 `gemm` operator,
  *                                                                              Sec. 4.1 workloads)
  *
+ * and the parts of a mixture-of-experts layer: its grouped GEMMs (axe_gemm_grouped, axe_gemm_grouped_pair) and what stands around them (axe_rmsnorm,
+ * axe_route, axe_rows_dispatch, axe_rows_combine, and their gradients).
+ *
  * Conventions common to all entry points
  *   - Pointers named d_* are DEVICE pointers (HIP global memory on the current device); every
  *     other pointer is a HOST pointer.  The caller owns all of them; descriptors are read during
@@ -19,7 +22,7 @@
  *     returned.  No call aborts or throws.  axe_strerror() names a code, axe_last_error() gives
  *     the detailed message of the calling thread's last failure.
  *   - The library keeps no mutable state apart from thread-local ones -- that message, and the plan of the
- *     thread's last axe_gemm, axe_relayout and axe_layout_eval, used again when the next call's descriptor is
+ *     thread's last axe_gemm, axe_relayout, axe_layout_eval and of each of the calls around the grouped GEMMs, used again when the next call's descriptor is
  *     the same word by word -- and allocates no device memory.
  *   - One GPU holds the whole tensor: an axis other than the memory axis may appear only with
  *     total extent 1 (e.g. the extent-1 `gpuid` iter and `gpuid` offset of one shard of a

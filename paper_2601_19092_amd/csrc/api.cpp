@@ -132,7 +132,7 @@ int check_relayout_pointers(int32_t elem_bytes, const void* d_src, int64_t src_e
 
 extern "C" {
 
-int32_t axe_version(void) { return 10300; }   // 1.3.0: grouped GEMM, fp16, blocked operands, per-row scales (descriptor fields added)
+int32_t axe_version(void) { return 10400; }   // 1.4.0: norm, routing and rows around the grouped GEMMs (1.3.0: grouped GEMM, fp16, blocked operands, per-row scales)
 
 const char* axe_strerror(int code) {
   switch (code) {

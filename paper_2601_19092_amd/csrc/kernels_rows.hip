@@ -126,13 +126,14 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
   store_run(v, elem_at(a.to_tokens, w.t * a.ldt, EB), w.c, a.H);
 }
 
-// A wave per pair, RUNS runs of a lane at a time.  DOT: the rows are read, for dweights.  PAST: what goes past the caches, 1: stores, 2: loads of the rows, too.
+// A wave per pair, eight to a workgroup (the pairs of a token read its row together: with four, and two workgroups on different XCDs, 4096 tokens of 8 rows fetched 170 MB for 151),
+// RUNS runs of a lane at a time.  DOT: the rows are read, for dweights.  PAST: what goes past the caches, 1: stores, 2: loads of the rows, too.
 template <int TYPE, int RUNS, bool DOT, int PAST, bool SHORT>
-__global__ __launch_bounds__(256) void rows_combine_backward_kernel(RowsArgs a) {
+__global__ __launch_bounds__(512) void rows_combine_backward_kernel(RowsArgs a) {
   fetch_arguments(a.tokens, a.row_of, a.H);
   constexpr int EB = elem_bytes(TYPE);
   const int lane = threadIdx.x & 63;
-  const int64_t pair = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t pair = (int64_t)blockIdx.x * 8 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (pair >= a.T * a.k) return;
   const int64_t t = pair / a.k;
   const int64_t r = a.row_of[pair];
@@ -251,11 +252,12 @@ hipError_t launch_rows_combine(const RowsArgs& a, hipStream_t s) {
 
 template <int TYPE, bool DOT, int PAST>
 hipError_t launch_combine_backward(const RowsArgs& a, hipStream_t s) {
-  return in_pieces(a, a.k, [&](const RowsArgs& p, uint32_t groups) {
-    if (a.H < 8) rows_combine_backward_kernel<TYPE, 1, DOT, 0, true><<<groups, 256, 0, s>>>(p);
-    else if (a.H <= kSlab) rows_combine_backward_kernel<TYPE, 1, DOT, PAST, false><<<groups, 256, 0, s>>>(p);
-    else if (a.H <= 2 * kSlab) rows_combine_backward_kernel<TYPE, 2, DOT, PAST, false><<<groups, 256, 0, s>>>(p);
-    else rows_combine_backward_kernel<TYPE, 4, DOT, PAST, false><<<groups, 256, 0, s>>>(p);
+  return in_pieces(a, a.k, [&](const RowsArgs& p, uint32_t) {
+    const uint32_t groups = (uint32_t)((p.T * p.k + 7) / 8);
+    if (a.H < 8) rows_combine_backward_kernel<TYPE, 1, DOT, 0, true><<<groups, 512, 0, s>>>(p);
+    else if (a.H <= kSlab) rows_combine_backward_kernel<TYPE, 1, DOT, PAST, false><<<groups, 512, 0, s>>>(p);
+    else if (a.H <= 2 * kSlab) rows_combine_backward_kernel<TYPE, 2, DOT, PAST, false><<<groups, 512, 0, s>>>(p);
+    else rows_combine_backward_kernel<TYPE, 4, DOT, PAST, false><<<groups, 512, 0, s>>>(p);
   });
 }
 template <bool DOT, int PAST>

@@ -109,8 +109,8 @@ def synthetic(tokens: int, fp8: bool, hidden: int = W.MOE_HIDDEN, inter: int = W
 def main(argv) -> None:
     import torch
 
-    def us(f, n=50):
-        for _ in range(10):
+    def us(f, n=200):
+        for _ in range(100):
             f()
         a, b = torch.cuda.Event(True), torch.cuda.Event(True)
         a.record()
