@@ -262,10 +262,14 @@ struct Max {
 // v of all 16 lanes of a row, or of 32, or of all 64, joined, in every lane.  (Each step joins lanes that hold the same number of values: the
 // two sides of a step are the same in both lanes, so the results are the same bits.)
 template <class OP>
-__device__ __forceinline__ float row16_all(float v) {
+__device__ __forceinline__ float row8_all(float v) {               // eight lanes
   v = OP::of(v, __int_as_float(dpp<kXor1>(__float_as_int(v))));
   v = OP::of(v, __int_as_float(dpp<kXor2>(__float_as_int(v))));
-  v = OP::of(v, __int_as_float(dpp<kHalfMirror>(__float_as_int(v))));
+  return OP::of(v, __int_as_float(dpp<kHalfMirror>(__float_as_int(v))));
+}
+template <class OP>
+__device__ __forceinline__ float row16_all(float v) {
+  v = row8_all<OP>(v);
   return OP::of(v, __int_as_float(dpp<kMirror>(__float_as_int(v))));
 }
 template <class OP>
