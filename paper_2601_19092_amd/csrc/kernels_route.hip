@@ -140,12 +140,11 @@ __device__ __forceinline__ int scan_in_place(int* x, int n) {
 
 // LDS: masks and running counts, the choices of 64 tokens with what they were chosen by, and for each token at work its scores (with a bias) and what its groups need.
 struct RouteLds {
-  int run, key, chosen, tokens, token_words;                       // byte offsets; words of a token
+  int run, chosen, tokens, token_words;                       // byte offsets; words of a token
   __host__ __device__ RouteLds(const RouteArgs& a, int lanes_experts, bool logits, bool groups) {
     run = a.E * 8;
-    key = run + a.E * 4;
-    chosen = key + kMaskTokens * a.k * 4;
-    tokens = (chosen + kMaskTokens * a.k * 2 + 15) / 16 * 16;
+    chosen = (run + a.E * 4 + 7) / 8 * 8;
+    tokens = (chosen + kMaskTokens * a.k * 8 + 15) / 16 * 16;
     token_words = (logits || !a.bias ? 0 : lanes_experts) + (groups ? lanes_experts + 2 * a.groups : 0);
     token_words = (token_words + 3) / 4 * 4;
   }
@@ -175,13 +174,14 @@ __device__ __forceinline__ void join_two(float& first, float& second) {
 }
 
 // Strikes out the experts of the groups that do not stay.  by: what the lane's experts' groups are judged by (-inf: masked).  Groups of 1, 2, 4, ... whole lanes are judged in
-// registers, others through LDS.
-template <int LPT, int V>
+// registers (kWholeLanes), others through LDS.  (Kernels of their own: what the compiler prepares for the one costs the other registers and a microsecond.)
+constexpr int kNoGroups = 0, kWholeLanes = 1, kAnyGroups = 2;
+template <int LPT, int V, int GROUPS>
 __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, int e0, const float (&by)[V], int (&key)[V], float* mine) {
   const int per = a.per;
   const float none = -__builtin_inff();
-  const int lanes = per / V;                                       // of a group (V is a power of two)
-  if (per == lanes * V && (lanes & (lanes - 1)) == 0) {
+  if constexpr (GROUPS == kWholeLanes) {
+    const int lanes = per / V;                                     // of a group
     float first = none, second = none;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -299,14 +299,14 @@ __device__ __forceinline__ int first_lane(bool mine) {
 
 // LOGITS: softmax without a bias, chosen by the logits themselves.  tokens: of a workgroup.  With the order: places inside the block to row_of and the block's counts to the
 // workspace, or, alone, the whole order.
-template <int XT, int LPT, int V, bool LOGITS, bool GROUPS, bool SHORT>
+template <int XT, int LPT, int V, bool LOGITS, int GROUPS, bool SHORT>
 __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bool alone, int counts_pitch) {
   fetch_arguments(a.logits, a.T, a.scale);
   extern __shared__ char mem[];
-  const RouteLds at(a, LPT * V, LOGITS, GROUPS);
+  const RouteLds at(a, LPT * V, LOGITS, GROUPS == kAnyGroups);
   uint64_t* mask = (uint64_t*)mem;
-  int *run = (int*)(mem + at.run), *keys = (int*)(mem + at.key);   // run: the expert's pairs in the block's tokens before these
-  uint16_t* chosen = (uint16_t*)(mem + at.chosen);
+  int* run = (int*)(mem + at.run);                                 // the expert's pairs in the block's tokens before these
+  int2* chosen = (int2*)(mem + at.chosen);                         // expert (-1: none) and what it was chosen by
   float* own_scores = (float*)(mem + at.tokens) + threadIdx.x / LPT * at.token_words;
   float* by_group = own_scores + (LOGITS || !a.bias ? 0 : LPT * V);
   const int tid = threadIdx.x, threads = blockDim.x, lane = tid % LPT;
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
           float by[V];                                             // (scores up to a common factor)
 #pragma unroll
           for (int v = 0; v < V; ++v) by[v] = key[v] == kNone ? none : a.top2 ? exp_of(x.l[v] - m) : x.l[v];
-          keep_groups<LPT, V>(a, lane, x.e0, by, key, by_group);
+          keep_groups<LPT, V, GROUPS>(a, lane, x.e0, by, key, by_group);
         }
       } else {
         float s[V];
@@ -374,23 +374,20 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
           s[v] = x.l[v] > none && s[v] > none ? s[v] + 0.0f : none;  // (NaN compares false)
           key[v] = key_of(s[v]);
         }
-        if (GROUPS) keep_groups<LPT, V>(a, lane, x.e0, s, key, by_group);
+        if (GROUPS) keep_groups<LPT, V, GROUPS>(a, lane, x.e0, s, key, by_group);
       }
       // k times the largest of the lanes' first ones; of lanes that have it, the first; that lane notes the choice down
       Lists<V> list(key);
       for (int j = 0; j < a.k; ++j) {
         const int first = list.first(), best = all_int<LPT, IMax>(first);
         const bool mine = lane == first_lane<LPT>(first == best);
-        if (mine) {
-          chosen[i * a.k + j] = best == kNone ? 0xffff : (uint16_t)(x.e0 + list.index());
-          keys[i * a.k + j] = best;
-        }
+        if (mine) chosen[i * a.k + j] = int2{best == kNone ? -1 : x.e0 + list.index(), best};
         list.drop(mine);
       }
       token_sync();
       // lane j: choice j and its weight (without a bias the key says what it was chosen by)
-      const int id = lane < a.k ? (int)(int16_t)chosen[i * a.k + lane] : -1;
-      const int by = lane < a.k ? keys[i * a.k + lane] : kNone;
+      const int2 mine = lane < a.k ? chosen[i * a.k + lane] : int2{-1, kNone};
+      const int id = mine.x, by = mine.y;
       float w = 0;
       if (LOGITS && a.renorm && !(GROUPS && a.top2)) m = value_of(all_int<LPT, IMax>(by));         // (no choice: not a number, and not used)
       if (id >= 0) w = LOGITS ? exp_of(value_of(by) - m) : a.bias ? own_scores[id] : value_of(by);
@@ -404,8 +401,8 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
     if (!order) continue;
     lds_barrier();
     for (int p = tid; p < n * a.k; p += threads) {
-      const uint16_t e = chosen[p];
-      if (e != 0xffff) atomicOr((unsigned long long*)&mask[e], 1ull << (p / a.k));
+      const int e = chosen[p].x;
+      if (e >= 0) atomicOr((unsigned long long*)&mask[e], 1ull << (p / a.k));
     }
     lds_barrier();
     if (alone) {                                                   // (one mask: run becomes where the expert's rows begin)
@@ -419,9 +416,9 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
       for (int e = tid; e < a.E; e += threads) a.group_rows[e] = run[e];
     }
     for (int p = tid; p < n * a.k; p += threads) {
-      const uint16_t e = chosen[p];
+      const int e = chosen[p].x;
       const int i = p / a.k;
-      a.row_of[s0 * a.k + p] = e == 0xffff ? -1 : run[e] + __popcll(mask[e] & ((1ull << i) - 1));
+      a.row_of[s0 * a.k + p] = e < 0 ? -1 : run[e] + __popcll(mask[e] & ((1ull << i) - 1));
     }
     if (alone) return;
     lds_barrier();
@@ -605,18 +602,22 @@ void launch_route_of(const RouteArgs& a, hipStream_t s) {
     const int tokens = alone ? kMaskTokens : block_tokens(a.T), pitch = counts_pitch(a.E), blocks = (int)((a.T + tokens - 1) / tokens);
     const int here = (int)(a.T < tokens ? a.T : tokens);
     auto launch = [&](auto logits, auto groups) {
-      constexpr bool L = decltype(logits)::value, G = decltype(groups)::value;
-      const RouteLds lds(a, S::LPT * S::V, L, G);
+      constexpr bool L = decltype(logits)::value;
+      constexpr int G = decltype(groups)::value;
+      const RouteLds lds(a, S::LPT * S::V, L, G == kAnyGroups);
       // tokens at once: all of a mask's, as far as threads and LDS go
       int n = std::min(1024, (std::min(here, kMaskTokens) * S::LPT + 63) / 64 * 64);
       while (n > 64 && lds.tokens + n / S::LPT * lds.token_words * 4 > 65536) n = (n / 2 + 63) / 64 * 64;
       route_kernel<XT, S::LPT, S::V, L, G, S::SHORT><<<blocks, n, lds.tokens + n / S::LPT * lds.token_words * 4, s>>>(a, tokens, alone, pitch);
     };
-    using Yes = std::true_type;
-    using No = std::false_type;
-    const bool logits = !a.sigmoid && !a.bias;
-    if (a.groups > 1) logits ? launch(Yes(), Yes()) : launch(No(), Yes());
-    else logits ? launch(Yes(), No()) : launch(No(), No());
+    auto by_groups = [&](auto logits) {
+      const int lanes = a.per / S::V;
+      if (a.groups == 1) launch(logits, std::integral_constant<int, kNoGroups>());
+      else if (!S::SHORT && a.per == lanes * S::V && (lanes & (lanes - 1)) == 0) launch(logits, std::integral_constant<int, S::SHORT ? kAnyGroups : kWholeLanes>());
+      else launch(logits, std::integral_constant<int, kAnyGroups>());
+    };
+    if (!a.sigmoid && !a.bias) by_groups(std::true_type());
+    else by_groups(std::false_type());
     if (a.row_of && !alone) launch_order<1>(a, tokens, blocks, pitch, s);
   });
 }
