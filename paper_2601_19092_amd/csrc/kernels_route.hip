@@ -5,7 +5,7 @@
 // then the first lane that has it), whose owner notes it down and moves its list up: some 170 ns each.  Choices are compared as integers of the same order as the numbers.
 //
 // The experts' order is a stable counting sort.  A workgroup has a block of consecutive tokens, 64 at a time, as bits of one 64-bit mask per expert in LDS: whatever the order
-// in which the bits arrive, the number of set bits below a token's is its place among the expert's pairs.  Up to 32 to 64 tokens are one workgroup, which goes on to add up the
+// in which the bits arrive, the number of set bits below a token's is its place among the expert's pairs.  Few tokens (one_workgroup) are one workgroup, which goes on to add up the
 // experts.  More leave places inside the block and the block's count per expert (16 bits) behind; a second kernel, a workgroup per block, adds up the counts of
 // all blocks (its own share of that work is small, and there is nothing to wait for) and moves the places to where expert and block begin.
 #include <hip/hip_runtime.h>
@@ -140,7 +140,7 @@ __device__ __forceinline__ int scan_in_place(int* x, int n) {
 
 // LDS: masks and running counts, the choices of 64 tokens with what they were chosen by, and for each token at work its scores (with a bias) and what its groups need.
 struct RouteLds {
-  int run, chosen, tokens, token_words;                       // byte offsets; words of a token
+  int run, chosen, tokens, token_words;                            // byte offsets; words of a token
   __host__ __device__ RouteLds(const RouteArgs& a, int lanes_experts, bool logits, bool groups) {
     run = a.E * 8;
     chosen = (run + a.E * 4 + 7) / 8 * 8;
@@ -210,7 +210,7 @@ __device__ __forceinline__ void keep_groups(const RouteArgs& a, int lane, int e0
   }
   float* score = mine + LPT * V;
   int* keep = (int*)(score + a.groups);
-  token_sync();                                                     // (the token before has been read)
+  token_sync();                                                    // (the token before has been read)
 #pragma unroll
   for (int v = 0; v < V; ++v) mine[e0 + v] = by[v];                // (room for all lanes' experts, those that are none too)
   token_sync();
@@ -302,7 +302,7 @@ __device__ __forceinline__ int first_lane(bool mine) {
 template <int XT, int LPT, int V, bool LOGITS, int GROUPS, bool SHORT>
 __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bool alone, int counts_pitch) {
   fetch_arguments(a.logits, a.T, a.scale);
-  extern __shared__ char mem[];
+  extern __shared__ __align__(16) char mem[];
   const RouteLds at(a, LPT * V, LOGITS, GROUPS == kAnyGroups);
   uint64_t* mask = (uint64_t*)mem;
   int* run = (int*)(mem + at.run);                                 // the expert's pairs in the block's tokens before these
