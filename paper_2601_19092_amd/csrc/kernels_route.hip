@@ -42,9 +42,6 @@ __device__ __forceinline__ float value_of(int key) { return __int_as_float(key ^
 struct IMax {
   __device__ __forceinline__ static int of(int a, int b) { return max(a, b); }
 };
-struct IMin {
-  __device__ __forceinline__ static int of(int a, int b) { return min(a, b); }
-};
 template <int LPT, class OP>
 __device__ __forceinline__ int all_int(int v) {
   v = OP::of(v, dpp<kXor1>(v));
