@@ -344,8 +344,8 @@ int axe_gemm_grouped_pair_static(const axe_gemm_grouped_desc_t* g1, const axe_ge
  *   d_w : H weights of weight_dtype (one of the same three), or NULL: ones.
  *   y : (T, H) of y_dtype: x_dtype; AXE_BF16 or AXE_F16 of AXE_F32 rows; or AXE_FP8_E4M3 with d_scales row-major (T, ceil(H / 128)),
  *       fp32 or E8M0 by scale_dtype, one scale per row and 128 columns, which is what axe_gemm (scale_a_rows = 1) and axe_gemm_grouped read:
- *           q = e4m3(y / s), round to nearest even,   fp32: s = max(|y|) / 448, at least 2^-126;   E8M0: the smallest power of two not below
- *           max(|y|) / 448, at least 2^-126;   s = 1 where all of the 128 are 0.
+ *           q = e4m3(y / s), round to nearest even (of y / s in fp32, itself rounded so),   fp32: s = max(|y|) / 448, at least 2^-126;
+ *           E8M0: the smallest power of two not below max(|y|) / 448, at least 2^-126;   s = 1 where all of the 128 are 0.
  *       NaNs are left out of the maximum and stay NaN; an infinite maximum counts as the largest fp32 number, infinities become +-448.
  *       (axe_gemm_grouped reads E8M0 codes in words: pad that allocation to a multiple of 4 bytes.)
  *       d_y may be d_x or d_residual with the same layout and element size.

@@ -66,8 +66,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rmsnorm_kernel(NormArgs
 #pragma unroll
       for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(y[k]));  // (NaN: the other operand)
       const Scale s = scale_of(row16_all<Max>(most), a.e8m0);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] *= s.inv;
+      over_scale(y, s);
       if ((threadIdx.x & 15) == 0 && ci < a.H) store_scale(a.scales, t * ((a.H + 127) >> 7) + (ci >> 7), s, a.e8m0);
     }
     q.set(y);

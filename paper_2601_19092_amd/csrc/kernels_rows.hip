@@ -87,8 +87,7 @@ __global__ __launch_bounds__(256) void rows_quantise_kernel(RowsArgs a) {
   Run8<kFp8> q[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) y[i][k] *= s.inv;
+    over_scale(y[i], s);
     q[i].set(y[i]);
   }
   const int blocks = (a.H + 127) >> 7;
