@@ -378,10 +378,11 @@ int64_t axe_rmsnorm_workspace(const axe_rmsnorm_desc_t* g);   /* words, or a neg
  *   groups > 1: the E / groups consecutive experts of a group stand or fall together; a group's score is its largest choice
  *   (AXE_ROUTE_GROUP_MAX) or the sum of its two largest (AXE_ROUTE_GROUP_TOP2), and the groups_kept best groups stay (groups up to 64, a divisor of E).
  *   d_ids (T, k) int32: the k largest choices of what is left, largest first, equal ones lowest index first (experts and groups).
- *   d_weights (T, k) fp32: scale * s of the chosen, divided by their sum if renorm (0 if that sum is 0).  The bias does not enter.
+ *   d_weights (T, k) fp32: scale * s of the chosen, divided by their sum if renorm (0 if that sum is 0; a sigmoid below e^-700 counts as 0, others keep their ratios however small
+ *   they are).  The bias does not enter.
  *   Masked experts: a logit of -inf or NaN, or a choice of -inf or NaN, is never chosen; its softmax score is 0.  A row with fewer than k experts left has id -1, weight 0
  *   in the places that remain (all of them, if it leaves none).  The lowest finite value of a type is no mask: such experts come last.  +inf counts as the largest fp32 number.
- *   Without bias, softmax choices are compared by their logits (the same order, no rounding).
+ *   Without bias, choices are compared by their logits (the same order, no rounding); with one, and the sums of AXE_ROUTE_GROUP_TOP2, as fp32 numbers.
  *   The experts' order (both given or both NULL): d_group_rows (E + 1) int32, what axe_gemm_grouped reads: expert e has the rows group_rows[e] ..
  *   group_rows[e+1]-1; d_row_of (T, k) int32: the row of (t, j), by expert, then token; -1 where the id is -1.  T k < 2^31.
  *   d_ws, ws_elems : workspace of axe_route_workspace(g) 4-byte words (0 for small T), owned by the caller, overwritten; needed with the order only.

@@ -32,6 +32,20 @@ __device__ __forceinline__ float exp_of(float x) {
   return t < 128.0f ? fmaf(p, d * 0.6931471805599453f, p) : p;
 }
 __device__ __forceinline__ float sigmoid(float l) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-l)); }   // (the reciprocal, too)
+// The same down to the smallest subnormal number (the hardware's 2^t ends at the smallest normal one): e^-64 = 1.60381089e-28.
+__device__ __forceinline__ float exp_below(float x) {
+  const bool far = x < -64.0f;
+  return exp_of(far ? x + 64.0f : x) * (far ? 1.60381089e-28f : 1.0f);
+}
+// The score that a weight is made of.  softmax: exp of how far the logit l is below `largest`.  sigmoid: where `largest` is below 0, that much larger than it is.  With the chosen experts' largest
+// logit the largest score of a token is at least 1/2, however small it is itself, and so is the sum that the weights are divided by; without that division `largest` is the row's, or 0.  A sigmoid
+// below e^-700 counts as 0: a row whose logits are all the lowest finite value gets no weights.
+constexpr float kLowestLogit = -700.0f;
+__device__ __forceinline__ float score_of(float l, float largest, bool sigmoid) {
+  if (!sigmoid) return exp_below(l - largest);
+  const float s = exp_below(fminf(l, 0.0f) - fminf(largest, 0.0f)) * __builtin_amdgcn_rcpf(1.0f + exp_of(-fabsf(l)));
+  return l < kLowestLogit ? 0.0f : s;
+}
 // Integers in the order of numbers above -inf, and back; -inf and NaN: none.
 __device__ __forceinline__ int key_of(float v) {
   const int b = __float_as_int(v);
@@ -135,14 +149,14 @@ __device__ __forceinline__ int scan_in_place(int* x, int n) {
   return all;
 }
 
-// LDS: masks and running counts, the choices of 64 tokens with what they were chosen by, and for each token at work its scores (with a bias) and what its groups need.
+// LDS: masks and running counts, the choices of 64 tokens with what they were chosen by, and for each token at work its logits (with a bias) and what its groups need.
 struct RouteLds {
   int run, chosen, tokens, token_words;                            // byte offsets; words of a token
   __host__ __device__ RouteLds(const RouteArgs& a, int lanes_experts, bool logits, bool groups) {
     run = a.E * 8;
     chosen = (run + a.E * 4 + 7) / 8 * 8;
     tokens = (chosen + kMaskTokens * a.k * 8 + 15) / 16 * 16;
-    token_words = (logits || !a.bias ? 0 : lanes_experts) + (groups ? lanes_experts + 2 * a.groups : 0);
+    token_words = (logits ? 0 : lanes_experts) + (groups ? lanes_experts + 2 * a.groups : 0);
     token_words = (token_words + 3) / 4 * 4;
   }
 };
@@ -294,7 +308,7 @@ __device__ __forceinline__ int first_lane(bool mine) {
   return row ? __builtin_ctz(row) : 64;
 }
 
-// LOGITS: softmax without a bias, chosen by the logits themselves.  tokens: of a workgroup.  With the order: places inside the block to row_of and the block's counts to the
+// LOGITS: without a bias, chosen by the logits themselves (both scores grow with them, but in fp32 not all of them: sigmoids of 18 and 19 are one number).  tokens: of a workgroup.  With the order: places inside the block to row_of and the block's counts to the
 // workspace, or, alone, the whole order.
 template <int XT, int LPT, int V, bool LOGITS, int GROUPS, bool SHORT>
 __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bool alone, int counts_pitch) {
@@ -304,8 +318,8 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
   uint64_t* mask = (uint64_t*)mem;
   int* run = (int*)(mem + at.run);                                 // the expert's pairs in the block's tokens before these
   int2* chosen = (int2*)(mem + at.chosen);                         // expert (-1: none) and what it was chosen by
-  float* own_scores = (float*)(mem + at.tokens) + threadIdx.x / LPT * at.token_words;
-  float* by_group = own_scores + (LOGITS || !a.bias ? 0 : LPT * V);
+  float* own_logits = (float*)(mem + at.tokens) + threadIdx.x / LPT * at.token_words;
+  float* by_group = own_logits + (LOGITS ? 0 : LPT * V);
   const int tid = threadIdx.x, threads = blockDim.x, lane = tid % LPT;
   const int64_t b0 = (int64_t)blockIdx.x * tokens, b1 = b0 + tokens < a.T ? b0 + tokens : a.T;
   const bool order = a.row_of != nullptr;
@@ -319,20 +333,17 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
     for (int i = tid / LPT; i < n; i += threads / LPT) {
       const int64_t t = s0 + i;
       float bias[LOGITS ? 1 : V];
-      if (!LOGITS && a.bias) {
+      if constexpr (!LOGITS) {
 #pragma unroll
         for (int v = 0; v < V; ++v) bias[v] = a.bias[min(lane * V + v, a.E - 1)];
-      } else if (!LOGITS) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) bias[v] = 0;
       }
       const Logits<XT, LPT, V, SHORT> x(a, elem_at(a.logits, t * a.ld, elem_bytes(XT)), lane);
-      // the row's largest, and the sum of exp behind it, where more than the chosen ones' own matter
+      // softmax: the row's largest, and the sum of exp behind it, where more than the chosen ones' own matter
       float m = 0, total = 1.0f;
       if (!a.sigmoid && (!LOGITS || !a.renorm || (GROUPS && a.top2))) m = x.top();
       int key[V];
       if constexpr (LOGITS) {
-        if (!a.renorm) {
+        if (!a.sigmoid && !a.renorm) {
           total = 0;
 #pragma unroll
           for (int v = 0; v < V; ++v) total += exp_of(x.l[v] - m);
@@ -341,9 +352,9 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
 #pragma unroll
         for (int v = 0; v < V; ++v) key[v] = key_of(x.l[v]);
         if (GROUPS) {
-          float by[V];                                             // (scores up to a common factor)
+          float by[V];                                             // (sums of scores up to a common factor)
 #pragma unroll
-          for (int v = 0; v < V; ++v) by[v] = key[v] == kNone ? none : a.top2 ? exp_of(x.l[v] - m) : x.l[v];
+          for (int v = 0; v < V; ++v) by[v] = key[v] == kNone ? none : !a.top2 ? x.l[v] : a.sigmoid ? sigmoid(x.l[v]) : exp_of(x.l[v] - m);
           keep_groups<LPT, V, GROUPS>(a, lane, x.e0, by, key, by_group);
         }
       } else {
@@ -352,19 +363,17 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
 #pragma unroll
           for (int v = 0; v < V; ++v) s[v] = sigmoid(x.l[v]);
         } else {
-          float sum = 0;
+          total = 0;
 #pragma unroll
-          for (int v = 0; v < V; ++v) sum += s[v] = exp_of(x.l[v] - m);
-          sum = all_float<LPT, Add>(sum);
-          const float inv = sum > 0 ? 1.0f / sum : 0.0f;
+          for (int v = 0; v < V; ++v) total += s[v] = exp_of(x.l[v] - m);
+          total = all_float<LPT, Add>(total);
+          const float inv = total > 0 ? 1.0f / total : 0.0f;
 #pragma unroll
           for (int v = 0; v < V; ++v) s[v] *= inv;
         }
-        if (a.bias) {                                              // (the chosen ones' scores are read back there)
-          token_sync();                                            // (the token before has read its own)
+        token_sync();                                              // (the token before has read its own)
 #pragma unroll
-          for (int v = 0; v < V; ++v) own_scores[x.e0 + v] = s[v];
-        }
+        for (int v = 0; v < V; ++v) own_logits[x.e0 + v] = x.l[v]; // (the chosen ones' are read back there)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           s[v] += bias[v];
@@ -382,12 +391,12 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int tokens, bo
         list.drop(mine);
       }
       token_sync();
-      // lane j: choice j and its weight (without a bias the key says what it was chosen by)
+      // lane j: choice j and its weight (without a bias the key is its logit)
       const int2 mine = lane < a.k ? chosen[i * a.k + lane] : int2{-1, kNone};
       const int id = mine.x, by = mine.y;
-      float w = 0;
-      if (LOGITS && a.renorm && !(GROUPS && a.top2)) m = value_of(all_int<LPT, IMax>(by));         // (no choice: not a number, and not used)
-      if (id >= 0) w = LOGITS ? exp_of(value_of(by) - m) : a.bias ? own_scores[id] : value_of(by);
+      const float l = LOGITS ? value_of(by) : id >= 0 ? own_logits[id] : none;
+      if (a.renorm) m = LOGITS ? value_of(all_int<LPT, IMax>(by)) : all_float<LPT, Max>(l);         // (no choice: not a number, or none, and not used)
+      float w = id >= 0 ? score_of(l, m, a.sigmoid) : 0.0f;
       if (a.renorm) total = all_float<LPT, Add>(w);
       w = total > 0 ? a.scale * (w / total) : 0.0f;
       if (lane < a.k) {
@@ -613,7 +622,7 @@ void launch_route_of(const RouteArgs& a, hipStream_t s) {
       else if (!S::SHORT && a.per == lanes * S::V && (lanes & (lanes - 1)) == 0) launch(logits, std::integral_constant<int, S::SHORT ? kAnyGroups : kWholeLanes>());
       else launch(logits, std::integral_constant<int, kAnyGroups>());
     };
-    if (!a.sigmoid && !a.bias) by_groups(std::true_type());
+    if (!a.bias) by_groups(std::true_type());
     else by_groups(std::false_type());
     if (a.row_of && !alone) launch_order<1>(a, tokens, blocks, pitch, s);
   });
