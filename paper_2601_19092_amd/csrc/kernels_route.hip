@@ -494,32 +494,41 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a) {
   const Logits<XT, LPT, V, SHORT> x(a, row, lane);
   int id = lane < a.k ? a.ids_in[t * a.k + lane] : -1;
   if (id >= a.E) id = -1;
-  float g = id >= 0 ? a.dweights[t * a.k + lane] * a.scale : 0.0f, own = 0;
-  const float m = a.sigmoid ? 0.0f : x.top();
-  float s[V], total = 1.0f;
-#pragma unroll
-  for (int v = 0; v < V; ++v) s[v] = a.sigmoid ? sigmoid(x.l[v]) : exp_of(x.l[v] - m);
-  if (!a.sigmoid) {
-    total = 0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) total += s[v];
-    total = all_float<LPT, Add>(total);
-  }
-  const float inv = total > 0 ? 1.0f / total : 0.0f;
+  float g = id >= 0 ? a.dweights[t * a.k + lane] * a.scale : 0.0f;
+  float l = -__builtin_inff();                                     // of choice `lane`
   if (id >= 0) {
     Run8<XT> one;
     one.load_part((const typename Run8<XT>::Elem*)row + id, 1);
-    const float l = as_logit(one.get(0));
-    own = a.sigmoid ? sigmoid(l) : exp_of(l - m) * inv;
+    l = as_logit(one.get(0));
   }
-  float along = 0;
-  if (a.renorm) {                                                  // (then the sum of s ds is 0)
-    const float sum = all_float<LPT, Add>(own);
-    const float share = sum > 0 ? 1.0f / sum : 0.0f;
-    const float mean = all_float<LPT, Add>(g * (own * share));
-    g = id >= 0 ? (g - mean) * share : 0.0f;
-  } else if (!a.sigmoid) {
-    along = all_float<LPT, Add>(g * own);
+  // The gradient is f_e (ds_e - along); ds: what the choices bring to their experts.
+  float f[V], along = 0;
+  if (a.renorm) {
+    // w_e (g_e - sum w g), for a sigmoid times 1 - s_e: of the weights, which are ordinary numbers however small the scores and their sum are
+    const float largest = all_float<LPT, Max>(l);
+    const float sc = l > -__builtin_inff() ? score_of(l, largest, a.sigmoid) : 0.0f;
+    const float total = all_float<LPT, Add>(sc), w = total > 0 ? sc / total : 0.0f;
+    g = w * (g - all_float<LPT, Add>(g * w));
+    if (a.sigmoid) g *= sigmoid(-l);
+#pragma unroll
+    for (int v = 0; v < V; ++v) f[v] = 1.0f;
+  } else if (a.sigmoid) {
+    // s (1 - s) = e / (1 + e)^2, e = exp(-|l|): without the difference, of which nothing is left from 17 on
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float e = exp_of(-fabsf(x.l[v])), r = __builtin_amdgcn_rcpf(1.0f + e);
+      f[v] = e * r * r;
+    }
+  } else {
+    const float m = x.top();
+    float total = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) total += f[v] = exp_of(x.l[v] - m);
+    total = all_float<LPT, Add>(total);
+    const float inv = total > 0 ? 1.0f / total : 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) f[v] *= inv;
+    along = all_float<LPT, Add>(id >= 0 ? g * (exp_of(l - m) * inv) : 0.0f);
   }
   float ds[V] = {};
   for (int j = 0; j < a.k; ++j) {
@@ -535,8 +544,7 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a) {
 #pragma unroll
     for (int k = 0; k < 8 && k < V; ++k) {
       const int v = 8 * i + k;
-      const float p = s[v] * inv;
-      d[k] = x.l[v] == -__builtin_inff() ? 0.0f : a.sigmoid ? s[v] * (1.0f - s[v]) * ds[v] : p * (ds[v] - along);
+      d[k] = x.l[v] == -__builtin_inff() ? 0.0f : f[v] * (ds[v] - along);
     }
     Run8<XT> r;
     r.set(d);

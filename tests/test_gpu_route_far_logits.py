@@ -112,3 +112,79 @@ def test_rows_of_the_lowest_value_get_no_sigmoid_weights():
         assert (w[1::2] == 0).all() and (ids[1::2] == np.arange(3)).all()
         if bias is None:
             assert (ids[::2, 0] == 5).all() and (w[::2] == [1.0, 0.0, 0.0]).all()
+
+
+# ---- gradients ------------------------------------------------------------------------------------------------------------------------------------
+# Unnormalised sigmoid: s (1 - s) g, three roundings more than two exponentials and reciprocals: 32 U of the value.  Renormalised: w (g - mean) (1 - s), w as above, the mean's error that of its
+# magnitudes: 96 U of w (1 - s) 2 max |g|.
+
+def gradient(logits, ids, g, dtype, score, renorm, scale=1.5):
+    T, E = logits.shape
+    d = B.RouteDesc(T, E, ids.shape[1], CODE[dtype], score=score, renorm=renorm, scale=scale)
+    out = torch.full((T, E), 7.0, dtype=TORCH[dtype], device="cuda")
+    B.axe_route_backward(d, logits.cuda(), torch.from_numpy(ids).int().cuda(), g.cuda(), out)
+    return f64(out)
+
+
+def other_side(l):
+    """1 - sigmoid(l) without cancellation."""
+    return 1.0 / (1.0 + np.exp(l))
+
+
+def exact_gradient(l, ids, g, score, renorm, scale=1.5):
+    """By the chosen logits, others 0: of renormalised weights, and of sigmoids."""
+    out = np.zeros_like(l)
+    c = np.take_along_axis(l, ids, 1)
+    if renorm:
+        top = c.max(1, keepdims=True)
+        w = np.exp(c - top) / (1 + np.exp(c) if score else 1.0)
+        w = w / w.sum(1, keepdims=True)
+        d = w * (scale * g - (w * scale * g).sum(1, keepdims=True)) * (other_side(c) if score else 1.0)
+    else:
+        d = scale * g * other_side(c) * other_side(-c)
+    np.put_along_axis(out, ids, d, 1)
+    return out
+
+
+@pytest.mark.parametrize("where", [(8.0, 20.0), (16.0, 60.0), (-95.0, -75.0), (-30.0, 30.0)])
+@pytest.mark.parametrize("T,E,k", [(1, 128, 8), (70, 16, 4), (40, 256, 8), (9, 1000, 12), (8200, 96, 5)])
+def test_sigmoid_gradient_far_out(T, E, k, where):
+    logits = spread_rows(T, E, *where, "f32", T)
+    ids = np.argsort(-f64(logits), axis=1, kind="stable")[:, :k]
+    g = torch.randn((T, k), generator=torch.Generator().manual_seed(1))
+    got, want = gradient(logits, ids, g, "f32", 1, False), exact_gradient(f64(logits), ids, f64(g), 1, False)
+    within(got, want, 32 * U * np.abs(want) + 2.0 ** -126, "dlogits")
+
+
+@pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("size", [1.0, 1e8])
+@pytest.mark.parametrize("where", [(8.0, 20.0), (-88.0, -80.0), (-95.0, -85.0), (-3.0, 3.0)])
+@pytest.mark.parametrize("T,E,k", [(1, 128, 8), (70, 16, 4), (40, 256, 8), (9, 1000, 12), (8200, 96, 5)])
+def test_renormalised_gradient_of_vanishing_scores(T, E, k, where, size, score):
+    """Gradients of ordinary size, and scaled ones, of weights whose scores' sum vanishes (softmax: next to other experts around 0)."""
+    logits = spread_rows(T, E, *where, "f32", T)
+    if score == 0:
+        logits[:, k:] = spread_rows(T, E - k, -1.0, 1.0, "f32", T + 1)
+    ids = np.arange(k)[None].repeat(T, 0)
+    g = size * torch.randn((T, k), generator=torch.Generator().manual_seed(1))
+    l, gv = f64(logits), f64(g)
+    got, want = gradient(logits, ids, g, "f32", score, True), exact_gradient(l, ids, gv, score, True)
+    c = l[:, :k]
+    top = c.max(1, keepdims=True)
+    w = np.exp(c - top) / (1 + np.exp(c) if score else 1.0)
+    mag = np.zeros_like(l)
+    mag[:, :k] = w / w.sum(1, keepdims=True) * (other_side(c) if score else 1.0) * 2 * 1.5 * np.abs(gv).max()
+    within(got, want, 96 * U * mag + 2.0 ** -126, "dlogits")
+
+
+def test_gradient_of_rows_that_leave_nothing_is_zero():
+    logits = torch.randn((70, 40), generator=torch.Generator().manual_seed(2))
+    logits[::3] = -float("inf")
+    ids = np.where(np.isneginf(f64(logits))[:, :5], -1, np.arange(5))
+    ids[3] = np.arange(5)                                              # (named, but masked)
+    for score in (0, 1):
+        for renorm in (True, False):
+            got = gradient(logits, ids, torch.ones((70, 5)), "f32", score, renorm)
+            assert (got[::3] == 0).all() and np.isfinite(got).all(), (score, renorm)
+            if not renorm:
+                assert (got[1, :5] != 0).all()
