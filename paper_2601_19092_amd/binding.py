@@ -416,15 +416,29 @@ def axe_gemm_grouped_describe(desc: GroupedGemmDesc, which: int) -> Tuple[dict, 
 
 
 # ---- around the experts' products: norm, routing, rows in the experts' order
-def _matrix(layout: Optional[Layout], rows: int, cols: int, elems: Optional[int], axis: str):
-    """A matrix operand: its layout (None: contiguous, row by row) and the elements of its buffer (None: as many as the layout reaches)."""
+# What a call takes of its operands is so many elements of so many bytes: the library is told the one and takes the other from the descriptor's types, so that what a tensor really is has to be
+# checked here.  An operand is described by (elements, bytes of one, whether it has no layout of its own: then it is contiguous, bytes of all).
+_BYTES = {AXE_BF16: 2, AXE_F16: 2, AXE_F32: 4, AXE_FP8_E4M3: 1}
+
+
+def _operand(elems: int, width: int, dense: bool = True):
+    return elems, width, dense, elems * width
+
+
+def _matrix(layout: Optional[Layout], rows: int, cols: int, elems: Optional[int], axis: str, dtype: int):
+    """A matrix operand: its layout (None: contiguous, row by row), the elements of its buffer (None: as many as the layout reaches) and its description."""
+    dense = layout is None
     if layout is None:
         layout = Layout({"D": [(max(rows, 1), cols, axis), (cols, 1, axis)]})
     if elems is None:
         a = layout.axis(axis)
         reach = sum((it.extent - 1) * it.stride for it in layout._d[:layout.c.n_d] if it.axis == a and it.stride > 0)
         elems = layout._o[a] + reach + 1 if rows else 0
-    return layout, elems
+    return layout, elems, _operand(elems, _BYTES.get(dtype, 0), dense)
+
+
+def _scale_bytes(scale_dtype: int) -> int:
+    return 1 if scale_dtype == AXE_SCALE_E8M0 else 4
 
 
 def _axis_of(axis: str, *layouts: Layout) -> int:
@@ -433,11 +447,20 @@ def _axis_of(axis: str, *layouts: Layout) -> int:
     return a
 
 
-def _ptr(t, elems: int = 0):
-    """The address of a device tensor that holds at least `elems` elements (None stays None)."""
+def _reach(t) -> int:
+    """Elements of a tensor's memory from its first one on."""
+    return 1 + sum((n - 1) * st for n, st in zip(t.shape, t.stride())) if t.numel() else 0
+
+
+def _ptr(t, operand):
+    """The address of a device tensor that holds such an operand (None stays None)."""
     if t is None:
         return None
-    assert t.is_cuda and t.numel() >= elems, "operands are device tensors of at least the elements that their layouts reach"
+    elems, width, dense, size = operand
+    if not (t.nbytes == size and t.is_contiguous() and t.is_cuda):     # (of the very size, as most are: fewer looks; the norm of one token 5.2 -> 4.9 us)
+        assert t.is_cuda and t.itemsize == width, "operands are device tensors whose elements have the size that the descriptor's type says"
+        assert t.numel() >= elems if t.is_contiguous() else not dense and _reach(t) >= elems, \
+            "operands hold the elements that their layouts reach, and are contiguous where they have no layout"
     return t.data_ptr()
 
 
@@ -464,20 +487,20 @@ class RmsNormDesc:
                  x: Optional[Layout] = None, residual: Optional[Layout] = None, sum: Optional[Layout] = None, y: Optional[Layout] = None,
                  x_elems: Optional[int] = None, residual_elems: Optional[int] = None, sum_elems: Optional[int] = None, y_elems: Optional[int] = None,
                  mem_axis: str = "m"):
-        m = [_matrix(L, T, H, n, mem_axis) for L, n in ((x, x_elems), (residual, residual_elems), (sum, sum_elems), (y, y_elems))]
-        self.layouts = tuple(L for L, _ in m)
+        m = [_matrix(L, T, H, n, mem_axis, dt) for L, n, dt in ((x, x_elems, x_dtype), (residual, residual_elems, x_dtype), (sum, sum_elems, x_dtype), (y, y_elems, y_dtype))]
+        self.layouts = tuple(L for L, _, _ in m)
         self.c = axe_rmsnorm_desc_t(T, H, x_dtype, y_dtype, weight_dtype, scale_dtype, eps, _axis_of(mem_axis, *self.layouts), *[L.c for L in self.layouts],
-                                    *[n for _, n in m])
+                                    *[n for _, n, _ in m])
         self.ref = C.byref(self.c)
-        self.elems = tuple(n for _, n in m)
+        self.elems = tuple(n for _, n, _ in m)
         self.scale_elems = T * (-(-H // 128))
+        self.operands = tuple(o for _, _, o in m) + (_operand(H, _BYTES.get(weight_dtype, 0)), _operand(self.scale_elems, _scale_bytes(scale_dtype)))
 
 
 def axe_rmsnorm(desc: RmsNormDesc, x, weight, y, residual=None, sum_out=None, scales=None, stream=None):
     """y = norm(x + residual) * weight; sum_out receives x + residual, scales those of an e4m3 y."""
-    ex, er, es, ey = desc.elems
-    rc = (_lib or lib()).axe_rmsnorm(desc.ref, _ptr(x, ex), _ptr(residual, er), _ptr(weight, desc.c.H), _ptr(sum_out, es), _ptr(y, ey), _ptr(scales, desc.scale_elems),
-                                     _stream_ptr(stream))
+    o_x, o_r, o_s, o_y, o_w, o_c = desc.operands
+    rc = (_lib or lib()).axe_rmsnorm(desc.ref, _ptr(x, o_x), _ptr(residual, o_r), _ptr(weight, o_w), _ptr(sum_out, o_s), _ptr(y, o_y), _ptr(scales, o_c), _stream_ptr(stream))
     if rc:
         _check(rc)
     return y
@@ -490,8 +513,8 @@ def axe_rmsnorm_workspace(desc: RmsNormDesc) -> int:
 
 def axe_rmsnorm_backward(desc: RmsNormDesc, dy, sum, weight, dx, dsum=None, dweight=None, workspace=None, stream=None):
     """Gradients of x (and of residual) and, with dweight, of the weights; `sum` is the normed rows, dsum what arrives at them otherwise."""
-    ex, er, es, ey = desc.elems
-    rc = (_lib or lib()).axe_rmsnorm_backward(desc.ref, _ptr(dy, ey), _ptr(sum, es), _ptr(weight, desc.c.H), _ptr(dsum, er), _ptr(dx, ex),
+    o_x, o_r, o_s, o_y, o_w, _ = desc.operands
+    rc = (_lib or lib()).axe_rmsnorm_backward(desc.ref, _ptr(dy, o_y), _ptr(sum, o_s), _ptr(weight, o_w), _ptr(dsum, o_r), _ptr(dx, o_x),
                                               _floats(dweight, desc.c.H), *_words(workspace), _stream_ptr(stream))
     if rc:
         _check(rc)
@@ -504,7 +527,7 @@ class RouteDesc:
     def __init__(self, T: int, E: int, k: int, logit_dtype: int = AXE_F32, score: int = AXE_ROUTE_SOFTMAX, renorm: bool = True, groups: int = 1,
                  groups_kept: int = 1, group_score: int = AXE_ROUTE_GROUP_MAX, scale: float = 1.0, bias=None, logits: Optional[Layout] = None,
                  logits_elems: Optional[int] = None, mem_axis: str = "m"):
-        L, n = _matrix(logits, T, E, logits_elems, mem_axis)
+        L, n, self.operand = _matrix(logits, T, E, logits_elems, mem_axis, logit_dtype)
         self.layouts, self.bias, self.elems, self.pairs = (L,), bias, n, T * k
         self.c = axe_route_desc_t(T, E, k, logit_dtype, score, int(bool(renorm)), groups, groups_kept, group_score, scale, L.axis(mem_axis), L.c, n,
                                   _floats(bias, E))
@@ -513,7 +536,7 @@ class RouteDesc:
 
 def axe_route(desc: RouteDesc, logits, ids, weights, group_rows=None, row_of=None, workspace=None, stream=None):
     """Chosen experts (int32) and weights (fp32) of every token; group_rows (int32, E + 1) and row_of (int32, as ids): the experts' order of the pairs."""
-    rc = (_lib or lib()).axe_route(desc.ref, _ptr(logits, desc.elems), _ints(ids, desc.pairs), _floats(weights, desc.pairs),
+    rc = (_lib or lib()).axe_route(desc.ref, _ptr(logits, desc.operand), _ints(ids, desc.pairs), _floats(weights, desc.pairs),
                                    _ints(group_rows, desc.c.E + 1), _ints(row_of, desc.pairs), *_words(workspace), _stream_ptr(stream))
     if rc:
         _check(rc)
@@ -527,8 +550,8 @@ def axe_route_workspace(desc: RouteDesc) -> int:
 
 def axe_route_backward(desc: RouteDesc, logits, ids, dweights, dlogits, stream=None):
     """Gradient of the logits from that of the weights."""
-    rc = (_lib or lib()).axe_route_backward(desc.ref, _ptr(logits, desc.elems), _ints(ids, desc.pairs), _floats(dweights, desc.pairs),
-                                            _ptr(dlogits, desc.elems), _stream_ptr(stream))
+    rc = (_lib or lib()).axe_route_backward(desc.ref, _ptr(logits, desc.operand), _ints(ids, desc.pairs), _floats(dweights, desc.pairs),
+                                            _ptr(dlogits, desc.operand), _stream_ptr(stream))
     if rc:
         _check(rc)
     return dlogits
@@ -540,17 +563,18 @@ class RowsDesc:
 
     def __init__(self, T: int, k: int, M: int, H: int, tokens_dtype: int, rows_dtype: int, scale_dtype: int = AXE_SCALE_F32, tokens: Optional[Layout] = None,
                  rows: Optional[Layout] = None, tokens_elems: Optional[int] = None, rows_elems: Optional[int] = None, mem_axis: str = "m"):
-        (Lt, nt), (Lr, nr) = _matrix(tokens, T, H, tokens_elems, mem_axis), _matrix(rows, M, H, rows_elems, mem_axis)
+        (Lt, nt, o_t), (Lr, nr, o_r) = _matrix(tokens, T, H, tokens_elems, mem_axis, tokens_dtype), _matrix(rows, M, H, rows_elems, mem_axis, rows_dtype)
         self.layouts, self.elems, self.pairs, self.nb = (Lt, Lr), (nt, nr), T * k, -(-H // 128)
+        sb = _scale_bytes(scale_dtype)
+        self.operands = o_t, o_r, _operand(T * self.nb, sb), _operand(M * self.nb, sb)
         self.c = axe_rows_desc_t(T, M, H, k, tokens_dtype, rows_dtype, scale_dtype, _axis_of(mem_axis, Lt, Lr), Lt.c, Lr.c, nt, nr)
         self.ref = C.byref(self.c)
 
 
 def axe_rows_dispatch(desc: RowsDesc, tokens, row_of, rows, token_scales=None, scales=None, stream=None):
     """rows[row_of[t][j]] = tokens[t], quantised where the rows are e4m3 (row_of None: the rows are in order already)."""
-    nt, nr = desc.elems
-    rc = (_lib or lib()).axe_rows_dispatch(desc.ref, _ptr(tokens, nt), _ptr(token_scales, desc.c.T * desc.nb), _ints(row_of, desc.pairs), _ptr(rows, nr),
-                                           _ptr(scales, desc.c.M * desc.nb), _stream_ptr(stream))
+    o_t, o_r, o_ts, o_rs = desc.operands
+    rc = (_lib or lib()).axe_rows_dispatch(desc.ref, _ptr(tokens, o_t), _ptr(token_scales, o_ts), _ints(row_of, desc.pairs), _ptr(rows, o_r), _ptr(scales, o_rs), _stream_ptr(stream))
     if rc:
         _check(rc)
     return rows
@@ -558,9 +582,8 @@ def axe_rows_dispatch(desc: RowsDesc, tokens, row_of, rows, token_scales=None, s
 
 def axe_rows_combine(desc: RowsDesc, rows, row_of, weights, tokens, add=None, stream=None):
     """tokens[t] = add[t] + sum_j weights[t][j] rows[row_of[t][j]] (weights None: ones)."""
-    nt, nr = desc.elems
-    rc = (_lib or lib()).axe_rows_combine(desc.ref, _ptr(rows, nr), _ints(row_of, desc.pairs), _floats(weights, desc.pairs), _ptr(add, nt),
-                                          _ptr(tokens, nt), _stream_ptr(stream))
+    o_t, o_r, _, _ = desc.operands
+    rc = (_lib or lib()).axe_rows_combine(desc.ref, _ptr(rows, o_r), _ints(row_of, desc.pairs), _floats(weights, desc.pairs), _ptr(add, o_t), _ptr(tokens, o_t), _stream_ptr(stream))
     if rc:
         _check(rc)
     return tokens
@@ -568,9 +591,9 @@ def axe_rows_combine(desc: RowsDesc, rows, row_of, weights, tokens, add=None, st
 
 def axe_rows_combine_backward(desc: RowsDesc, dtokens, rows, row_of, weights, drows=None, dweights=None, stream=None):
     """Gradients of the rows and of the weights from that of the tokens."""
-    nt, nr = desc.elems
-    rc = (_lib or lib()).axe_rows_combine_backward(desc.ref, _ptr(dtokens, nt), _ptr(rows, nr), _ints(row_of, desc.pairs),
-                                                   _floats(weights, desc.pairs), _ptr(drows, nr), _floats(dweights, desc.pairs),
+    o_t, o_r, _, _ = desc.operands
+    rc = (_lib or lib()).axe_rows_combine_backward(desc.ref, _ptr(dtokens, o_t), _ptr(rows, o_r), _ints(row_of, desc.pairs),
+                                                   _floats(weights, desc.pairs), _ptr(drows, o_r), _floats(dweights, desc.pairs),
                                                    _stream_ptr(stream))
     if rc:
         _check(rc)
