@@ -7,6 +7,7 @@
 #include "../../include/axe.h"
 #include "host_layout.h"
 #include "layer_ops.h"
+#include "layer_shapes.h"
 #include "plans.h"
 
 using namespace axe;

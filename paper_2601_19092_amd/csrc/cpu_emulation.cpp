@@ -346,8 +346,6 @@ hipError_t launch_route_backward(const RouteArgs&, hipStream_t) { return hipErro
 hipError_t launch_rows_dispatch(const RowsArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_rows_combine(const RowsArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_rows_combine_backward(const RowsArgs&, hipStream_t) { return hipErrorNotSupported; }
-int64_t rmsnorm_workspace_words(int64_t, int64_t) { return 0; }
-int64_t route_workspace_words(int64_t, int, int) { return 0; }
 
 }  // namespace axe
 

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include "layer_ops.h"
+#include "layer_shapes.h"
 #include "row_ops.h"
 
 namespace axe {
@@ -184,26 +185,6 @@ __global__ __launch_bounds__(256) void rmsnorm_no_rows_kernel(float* dw, int H) 
   if (blockIdx.x * 256 + threadIdx.x < (uint32_t)H) dw[blockIdx.x * 256 + threadIdx.x] = 0;
 }
 
-// Threads and runs of a row: as many threads as a run each needs, up to 512, then two and four runs.  Measured, us: 1000 x 8192 bf16 to e4m3 with 256 x 4 / 512 x 2 / 1024 x 1
-// 13.2 / 11.9 / 12.7, one row of 2048 with 64 x 4 / 256 x 1 3.4 / 2.3, fp16 2000 x 1999 6.0 / 5.8.  Backward, rows of a workgroup (of 512 or 1024 threads): it has
-// one row of the workspace to write for all of them; 4096 x 2048 bf16, 512 workgroups of 1 / 2 / 4 rows 16.1 / 14.6 / 13.6, 256 of 4 15.0, 1024 of 1 14.8.
-template <int TPR_, int RUNS_, bool SHORT_ = false>
-struct RowShape {
-  static constexpr int TPR = TPR_, RUNS = RUNS_, ROWS = TPR == 64 ? 8 : 1024 / TPR;
-  static constexpr bool SHORT = SHORT_;
-};
-template <class F>
-void by_row_shape(int H, F&& f) {
-  if (H < 8) f(RowShape<64, 1, true>());
-  else if (H <= 64 * 8) f(RowShape<64, 1>());
-  else if (H <= 128 * 8) f(RowShape<128, 1>());
-  else if (H <= 256 * 8) f(RowShape<256, 1>());
-  else if (H <= 512 * 8) f(RowShape<512, 1>());
-  else if (H <= 1024 * 8) f(RowShape<512, 2>());
-  else if (H <= 2048 * 8) f(RowShape<1024, 2>());
-  else f(RowShape<1024, 4>());
-}
-
 template <int XT, int YT>
 void launch_forward(const NormArgs& all, hipStream_t s) {
   // (a launch holds fewer than 2^32 threads)
@@ -233,18 +214,6 @@ hipError_t launch_rmsnorm(const NormArgs& a, hipStream_t s) {
   else if (a.y_type == kF16) launch_forward<kF32, kF16>(a, s);
   else launch_forward<kF32, kF32>(a, s);
   return hipGetLastError();
-}
-
-// Workgroups of the backward kernel: two for every compute unit, and one where it has at most two turns to make (a second launch costs more than they do).
-static int64_t backward_groups(int64_t T, int64_t H) {
-  int rows = 1;
-  by_row_shape((int)H, [&](auto shape) { rows = decltype(shape)::ROWS; });
-  const int64_t n = (T + rows - 1) / rows;
-  return n <= 2 ? (n ? 1 : 0) : n < 512 ? n : 512;
-}
-int64_t rmsnorm_workspace_words(int64_t T, int64_t H) {
-  const int64_t n = backward_groups(T, H);
-  return n > 1 ? n * H : 0;
 }
 
 template <int XT, int YT>

@@ -25,7 +25,6 @@ struct NormArgs {
 constexpr int64_t kNormMaxH = 32768;
 hipError_t launch_rmsnorm(const NormArgs& a, hipStream_t s);
 hipError_t launch_rmsnorm_backward(const NormArgs& a, hipStream_t s);
-int64_t rmsnorm_workspace_words(int64_t T, int64_t H);
 
 struct RouteArgs {
   const void* logits;
@@ -43,7 +42,6 @@ struct RouteArgs {
 constexpr int kRouteMaxE = 1024, kRouteMaxK = 64, kRouteMaxGroups = 64;
 hipError_t launch_route(const RouteArgs& a, hipStream_t s);
 hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s);
-int64_t route_workspace_words(int64_t T, int E, int k);
 
 // Bytes of a call from which its large operands go past the caches (non-temporal): they do not stay until they are touched again, and evicting for them costs time.  us, three sets of
 // buffers in turn.  Loads of combine's rows, cached / past: 2048 tokens of 8 rows of 2048 bf16 (72 MiB in all) 12.8 / 14.4, 3000 (105 MiB) 22.8 / 19.8, 4096 30.9 / 27.1.
