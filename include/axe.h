@@ -331,7 +331,7 @@ int axe_gemm_grouped_pair_static(const axe_gemm_grouped_desc_t* g1, const axe_ge
  * row (t, j) of the experts' order belongs to token t's j-th choice, M >= T k rows in all.
  *
  * Matrices carry layouts on `mem_axis` like the operands of axe_gemm: pitched, unit stride along the columns, no replicas, any offset and
- * any pitch of at least the columns (16-byte multiples are not required; they are faster); *_elems are the buffers' sizes in elements.
+ * any pitch of at least the columns (16-byte multiples are not required; they are faster); *_elems are the buffers' sizes in elements (at most 2^58).
  * Everything else is contiguous and row-major.  T = 0 is a call without rows: the layouts are not looked at, axe_route writes
  * group_rows = 0 and axe_rmsnorm_backward d_dweight = 0.
  * Buffers are aligned to their elements and outputs are disjoint from the inputs and from each other (AXE_EINVAL), but for what is said below.

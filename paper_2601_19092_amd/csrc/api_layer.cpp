@@ -50,10 +50,16 @@ int check_buffers(const char* fn, std::initializer_list<Buf> in, std::initialize
   return AXE_OK;
 }
 
-// One matrix of a call: its layout on the memory axis, planned once per descriptor.
+// One matrix of a call: its layout on the memory axis, planned once per descriptor.  Bytes of its buffer are computed of a matrix that was planned (or is not there) only: 64 bits hold them.
 struct Mat {
   int64_t ld = 0, off = 0;
 };
+constexpr int64_t kMostElems = int64_t(1) << 58;
+int plan_matrix(const axe_layout_t& L, int mem_axis, int64_t rows, int64_t cols, int64_t elems, const char* fn, Mat& m) {
+  if (elems > kMostElems) return invalid(fn, "a buffer of more than 2^58 elements");
+  return strided_2d(&L, mem_axis, rows, cols, true, elems, fn, &m.ld, &m.off);
+}
+int64_t bytes_of(const void* p, int64_t elems, int eb) { return p ? elems * eb : 0; }
 
 // The body of an entry point; planning allocates, and an entry point neither throws nor aborts.
 template <class F>
@@ -87,12 +93,12 @@ int check_norm(const axe_rmsnorm_desc_t* g, const char* fn, bool backward) {
   return AXE_OK;
 }
 int plan_norm(const axe_rmsnorm_desc_t* g, const char* fn, bool res, bool sum, NormPlan& p) {
-  if (int rc = strided_2d(&g->x, g->mem_axis, g->T, g->H, true, g->x_elems, fn, &p.x.ld, &p.x.off)) return rc;
-  if (int rc = strided_2d(&g->y, g->mem_axis, g->T, g->H, true, g->y_elems, fn, &p.y.ld, &p.y.off)) return rc;
+  if (int rc = plan_matrix(g->x, g->mem_axis, g->T, g->H, g->x_elems, fn, p.x)) return rc;
+  if (int rc = plan_matrix(g->y, g->mem_axis, g->T, g->H, g->y_elems, fn, p.y)) return rc;
   if (res)
-    if (int rc = strided_2d(&g->residual, g->mem_axis, g->T, g->H, true, g->residual_elems, fn, &p.r.ld, &p.r.off)) return rc;
+    if (int rc = plan_matrix(g->residual, g->mem_axis, g->T, g->H, g->residual_elems, fn, p.r)) return rc;
   if (sum)
-    if (int rc = strided_2d(&g->sum, g->mem_axis, g->T, g->H, true, g->sum_elems, fn, &p.s.ld, &p.s.off)) return rc;
+    if (int rc = plan_matrix(g->sum, g->mem_axis, g->T, g->H, g->sum_elems, fn, p.s)) return rc;
   return AXE_OK;
 }
 int kept_norm_plan(const axe_rmsnorm_desc_t* g, const char* fn, bool res, bool sum, NormPlan& out) {
@@ -142,7 +148,7 @@ int kept_route_plan(const axe_route_desc_t* g, const char* fn, Mat& out) {
     out = last.plan;
     return AXE_OK;
   }
-  if (int rc = strided_2d(&g->logits, g->mem_axis, g->T, g->E, true, g->logits_elems, fn, &out.ld, &out.off)) return rc;
+  if (int rc = plan_matrix(g->logits, g->mem_axis, g->T, g->E, g->logits_elems, fn, out)) return rc;
   if (keyed) last.keep(key, out);
   return AXE_OK;
 }
@@ -186,8 +192,8 @@ int kept_rows_plan(const axe_rows_desc_t* g, const char* fn, RowsPlan& out) {
     out = last.plan;
     return AXE_OK;
   }
-  if (int rc = strided_2d(&g->tokens, g->mem_axis, g->T, g->H, true, g->tokens_elems, fn, &out.t.ld, &out.t.off)) return rc;
-  if (int rc = strided_2d(&g->rows, g->mem_axis, g->M, g->H, true, g->rows_elems, fn, &out.r.ld, &out.r.off)) return rc;
+  if (int rc = plan_matrix(g->tokens, g->mem_axis, g->T, g->H, g->tokens_elems, fn, out.t)) return rc;
+  if (int rc = plan_matrix(g->rows, g->mem_axis, g->M, g->H, g->rows_elems, fn, out.r)) return rc;
   if (keyed) last.keep(key, out);
   return AXE_OK;
 }
@@ -212,8 +218,8 @@ int axe_rmsnorm(const axe_rmsnorm_desc_t* g, const void* d_x, const void* d_resi
     const int xb = elem_bytes(g->x_dtype), yb = elem_bytes(g->y_dtype), wb = elem_bytes(g->weight_dtype);
     const bool fp8 = g->y_dtype == AXE_FP8_E4M3;
     if (!fp8 && d_scales) return invalid(fn, "scales go with an e4m3 y");
-    Buf x = {d_x, g->x_elems * xb, xb, true}, r = {d_residual, g->residual_elems * xb, xb, false}, w = {d_w, g->H * wb, wb, false};
-    Buf s = {d_sum, g->sum_elems * xb, xb, false}, y = {d_y, g->y_elems * yb, yb, true};
+    Buf x = {d_x, g->x_elems * xb, xb, true}, r = {d_residual, bytes_of(d_residual, g->residual_elems, xb), xb, false}, w = {d_w, g->H * wb, wb, false};
+    Buf s = {d_sum, bytes_of(d_sum, g->sum_elems, xb), xb, false}, y = {d_y, g->y_elems * yb, yb, true};
     Buf sc = {d_scales, scale_bytes(g->T, g->H, g->scale_dtype), g->scale_dtype == AXE_SCALE_E8M0 ? 1 : 4, fp8};
     // In place: a thread reads what it needs of its elements before it writes them (and one that is written twice gets both, so not both outputs).
     Buf xi = x, ri = r;
@@ -255,7 +261,7 @@ int axe_rmsnorm_backward(const axe_rmsnorm_desc_t* g, const void* d_dy, const vo
     if (words > 0 && (!d_ws || ws_elems < words)) return invalid(fn, "the workspace is smaller than axe_rmsnorm_workspace");
     const bool any = g->T > 0;
     Buf dy = {d_dy, any ? g->y_elems * yb : 0, yb, any}, h = {d_sum, any ? g->sum_elems * xb : 0, xb, any}, w = {d_w, g->H * wb, wb, false};
-    Buf ds = {d_dsum, any ? g->residual_elems * xb : 0, xb, false}, dx = {d_dx, any ? g->x_elems * xb : 0, xb, any};
+    Buf ds = {d_dsum, any ? bytes_of(d_dsum, g->residual_elems, xb) : 0, xb, false}, dx = {d_dx, any ? g->x_elems * xb : 0, xb, any};
     Buf dw = {d_dweight, g->H * 4, 4, false}, ws = {words ? d_ws : nullptr, words * 4, 4, false};
     const bool on_dy = same(d_dx, p.x, xb, d_dy, p.y, yb), on_ds = same(d_dx, p.x, xb, d_dsum, p.r, xb);
     Buf dyi = dy, dsi = ds;
