@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) void rows_copy_scales_kernel(RowsArgs a, int b
   if (r >= 0 && r < a.M) ((S*)a.scales)[r * blocks + b] = ((const S*)a.token_scales)[t * blocks + b];
 }
 
-// Sixteen columns a lane: its store is 16 bytes (with eight and 8, us: 1024 tokens to 8 rows of 2048 6.7, now 5.9; 32768 rows of 768 in order 18.8, now 15.7).
+// Sixteen columns a lane: its store is 16 bytes (us, with eight and 8 / sixteen and 16: 1024 tokens to 8 rows of 2048 6.7 / 5.9, 32768 rows of 768 in order 18.8 / 15.7; with the codes of the quotient 6.1 and 16.3).
 template <int TYPE, bool SHORT>
 __global__ __launch_bounds__(256) void rows_quantise_kernel(RowsArgs a) {
   fetch_arguments(a.tokens, a.row_of, a.H);

@@ -47,7 +47,8 @@ hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s);
 // buffers in turn.  Loads of combine's rows, cached / past: 2048 tokens of 8 rows of 2048 bf16 (72 MiB in all) 12.8 / 14.4, 3000 (105 MiB) 22.8 / 19.8, 4096 30.9 / 27.1.
 // Its gradient's stores: 1024 (68 MiB) 12.8 / 12.8, 1500 (100 MiB) 20.6 / 17.6, 2048 30.4 / 23.4; its loads as well: 2048 (136 MiB) 23.4 / 27.7, 4096 (272 MiB) 56.2 / 52.4.  The norm's gradient's loads:
 // 4096 x 2048 (64 MiB) 13.4 / 15.8, 3000 x 8192 (188 MiB) 42.4 / 39.2, 4096 x 8192 55.9 / 53.0.  dispatch keeps its stores in the caches: past them 4096 tokens to e4m3 take
-// 14.7 for 15.4, but with the next kernel, which reads them, 45.4 for 41.4.
+// 14.7 for 15.4, but with the next kernel, which reads them, 45.4 for 41.4.  (The other lines are those of this loop: between the layer's products combine takes the same either way, and its gradient with a
+// reader of its rows behind it, one set of buffers, 2048 / 4096 / 8000 tokens, 33.7 / 81 / 157, all cached 31.5 / 66 / 172.)
 constexpr int64_t kPastCaches = int64_t(96) << 20, kReadsPastCaches = int64_t(128) << 20, kAllPastCaches = int64_t(256) << 20;
 
 struct RowsArgs {

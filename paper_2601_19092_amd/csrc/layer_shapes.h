@@ -45,7 +45,7 @@ inline int64_t rmsnorm_workspace_words(int64_t T, int64_t H) {
 constexpr int kMaskTokens = 64;                                    // tokens of a mask
 
 // Lanes of a token and experts of a lane: as many lanes as the experts fill while the tokens do not fill the chip (`few`: that many tokens), else fewer, whose lists are longer.  us,
-// 4096 tokens of 128 experts, 64 lanes x 2 / 16 x 8: 6.0 / 5.2, their gradient 4.4 / 5.1; one token 3.8 / 4.2; 1000 tokens of 256 experts with groups, 64 x 4 / 32 x 8: 7.8 / 8.2.  A
+// 4096 tokens of 128 experts, 64 lanes x 2 / 16 x 8: 6.0 / 5.2, their gradient 4.2 / 4.5; one token 3.8 / 4.2; 1000 tokens of 256 experts with groups, 64 x 4 / 32 x 8: 7.8 / 8.2.  A
 // workgroup that has all tokens to itself holds 16 of 64 lanes or 64 of 16 at once (whole calls, 128 experts: 16 tokens 5.6 / 5.8, 32 tokens 7.5 / 5.7, 64 tokens 11.9 / 7.0).
 template <int LPT_, int V_, bool SHORT_ = false>
 struct RouteShape {
