@@ -10,7 +10,7 @@
  *                                                                              Sec. 4.1 workloads)
  *
  * and the parts of a mixture-of-experts layer: its grouped GEMMs (axe_gemm_grouped, axe_gemm_grouped_pair) and what stands around them (axe_rmsnorm,
- * axe_route, axe_rows_dispatch, axe_rows_combine, and their gradients).
+ * axe_route, axe_rows_dispatch, axe_rows_combine, and their gradients); and of an attention layer, what stands between its products: axe_cache_append, axe_cache_attention.
  *
  * Conventions common to all entry points
  *   - Pointers named d_* are DEVICE pointers (HIP global memory on the current device); every
@@ -437,6 +437,53 @@ int axe_rows_combine(const axe_rows_desc_t* g, const void* d_rows, const int32_t
                      void* stream);
 int axe_rows_combine_backward(const axe_rows_desc_t* g, const void* d_dtokens, const void* d_rows, const int32_t* d_row_of, const float* d_weights,
                               void* d_drows, float* d_dweights, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Attention over a paged cache of keys and values, and the call that appends to the cache.
+ *
+ * S sequences.  The new tokens of all of them are the rows of q, k, v and out, one sequence after the other: sequence s has the rows seq_rows[s] .. seq_rows[s+1]-1, n of them,
+ * lengths[s] counts its tokens, the new ones among them, and its i-th row is the token at position lengths[s] - n + i.  The cache is `pages` pages of page_tokens tokens; position p of
+ * sequence s lies in page page_table[s][p / page_tokens], place p mod page_tokens.  All three arrays are int32 on the device, contiguous: d_seq_rows (S + 1), ascending,
+ * d_lengths (S), d_page_table (S, max_pages).  A page may stand in several rows of the table (a shared beginning), as long as no two new tokens have one place.
+ * What the arrays say is the device's to know, so it is not refused but bounded: a page outside [0, pages) holds nothing (what would go there is not stored, its keys are not seen), positions
+ * outside [0, max_pages page_tokens) have no place, lengths count as at most max_pages page_tokens and at least 0 where keys are seen, and rows that no sequence has are left as they are.
+ *
+ *   q, k, v, out     : (T, heads, head_dim) of dtype (AXE_BF16 or AXE_F16), any strides of tokens and heads, unit stride along the columns, no replicas; out also stands for the rotated queries.
+ *                      T counts the rows; seq_rows are taken as at most T.
+ *   k_cache, v_cache : (pages, page_tokens, kv_heads, head_dim) of cache_dtype, dtype or AXE_FP8_E4M3, in any order and with any gaps: unit stride along the columns, the other strides and the offset
+ *                      multiples of 8 elements, the address aligned to 8 elements.  e4m3: d_k_scales, d_v_scales (pages, page_tokens, kv_heads) fp32, contiguous; a row of a head is its codes times its scale.
+ *   q_heads          : a multiple of kv_heads, at most 128 times as many; head h reads head h / (q_heads / kv_heads) of the cache.
+ *   head_dim         : a multiple of 8 up to 256.  T, max_pages page_tokens and pages up to 2^30, S below 2^20, heads below 2^16.
+ *
+ * axe_cache_append -- cache[s, p] = (rot_p(k), v), q_out = rot_p(q) for every new token.
+ *   rot_p turns the first rotary_dim (even, up to head_dim, or 0) columns of a head in pairs, (a, b) -> (a cos - b sin, b cos + a sin): columns (i, i + rotary_dim / 2) (AXE_ROTATE_HALVES) or
+ *   (2 i, 2 i + 1) (AXE_ROTATE_PAIRS), by the cosine [p][i] and the sine [p][rotary_dim / 2 + i] of d_rotation, (max_pages page_tokens, rotary_dim) fp32, contiguous.
+ *   d_q and d_q_out (layouts q and out; q_out may be q with the same layout) are given together, or both NULL: keys and values alone.
+ *   In 32 bits, rounded once.  e4m3: s = max(|row|) / 448 over the head's columns, at least 2^-126, 1 where all are 0; codes as axe_rmsnorm makes them.
+ * axe_cache_attention -- out[t, h] = sum_j softmax_j(scale q[t, h] . K[j]) V[j] over the sequence's keys j < lengths[s] that the token at position p sees: causal: j <= p; window > 0 (causal
+ *   only): j > p - window, the token itself among them; otherwise all.  A token that sees no key: zeros.  scale from 2^-100 to 2^100.  Masked keys and values have no part in the result, whatever they hold
+ *   (NaN, infinities); a score of -inf counts as masked.  Scores, statistics and sums in 32 bits; the softmax's terms are rounded to dtype for the product with V.
+ *   d_ws, ws_elems : workspace of axe_cache_attention_workspace(g) 4-byte words (may be 0), owned by the caller, overwritten.
+ * Both may be captured into a graph and replayed with other contents of the three arrays: launches depend on the descriptor alone. */
+enum { AXE_ROTATE_HALVES = 0, AXE_ROTATE_PAIRS = 1 };
+typedef struct {
+  int64_t      T, pages;
+  int32_t      S, q_heads, kv_heads, head_dim;
+  int32_t      page_tokens, max_pages;
+  int32_t      dtype, cache_dtype;
+  int32_t      rotary_dim, rotary_style;      /* axe_cache_append */
+  int32_t      causal, window;                /* axe_cache_attention */
+  float        scale;
+  int32_t      mem_axis;
+  axe_layout_t q, k, v, out, k_cache, v_cache;
+  int64_t      q_elems, k_elems, v_elems, out_elems, k_cache_elems, v_cache_elems;
+} axe_cache_desc_t;
+
+int axe_cache_append(const axe_cache_desc_t* g, const void* d_q, const void* d_k, const void* d_v, const float* d_rotation, const int32_t* d_seq_rows, const int32_t* d_lengths,
+                     const int32_t* d_page_table, void* d_q_out, void* d_k_cache, void* d_v_cache, float* d_k_scales, float* d_v_scales, void* stream);
+int axe_cache_attention(const axe_cache_desc_t* g, const void* d_q, const void* d_k_cache, const void* d_v_cache, const float* d_k_scales, const float* d_v_scales,
+                        const int32_t* d_seq_rows, const int32_t* d_lengths, const int32_t* d_page_table, void* d_out, int32_t* d_ws, int64_t ws_elems, void* stream);
+int64_t axe_cache_attention_workspace(const axe_cache_desc_t* g);   /* words, or a negative error */
 
 /* ---------------------------------------------------------------------------------------------
  * axe_gemm_describe -- the Axe layouts of every tile movement of the kernel axe_gemm would

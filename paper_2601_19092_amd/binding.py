@@ -25,6 +25,7 @@ AXE_SCALE_F32, AXE_SCALE_E8M0 = 0, 1
 AXE_EPI_NONE, AXE_EPI_SWIGLU = 0, 1
 AXE_ROUTE_SOFTMAX, AXE_ROUTE_SIGMOID = 0, 1
 AXE_ROUTE_GROUP_MAX, AXE_ROUTE_GROUP_TOP2 = 0, 1
+AXE_ROTATE_HALVES, AXE_ROTATE_PAIRS = 0, 1
 AXE_GROUPED_AUTO, AXE_GROUPED_TILES, AXE_GROUPED_STREAM, AXE_GROUPED_TILES_256, AXE_GROUPED_TILES_128 = 0, 1, 2, 3, 4
 
 EXPORTS = ["axe_layout_eval", "axe_relayout", "axe_gemm", "axe_gemm_grouped", "axe_gemm_grouped_check", "axe_gemm_grouped_pair", "axe_gemm_grouped_pair_fused",
@@ -33,7 +34,8 @@ EXPORTS = ["axe_layout_eval", "axe_relayout", "axe_gemm", "axe_gemm_grouped", "a
            "axe_layout_equal", "axe_layout_group", "axe_layout_tile", "axe_layout_direct_sum", "axe_layout_flatten", "axe_layout_tile_of",
            "axe_layout_slice",
            "axe_rmsnorm", "axe_rmsnorm_backward", "axe_rmsnorm_workspace", "axe_route", "axe_route_backward", "axe_route_workspace",
-           "axe_rows_dispatch", "axe_rows_combine", "axe_rows_combine_backward"]
+           "axe_rows_dispatch", "axe_rows_combine", "axe_rows_combine_backward",
+           "axe_cache_append", "axe_cache_attention", "axe_cache_attention_workspace"]
 
 
 class axe_iter_t(C.Structure):
@@ -85,6 +87,14 @@ class axe_rows_desc_t(C.Structure):
     _fields_ = [("T", C.c_int64), ("M", C.c_int64), ("H", C.c_int64), ("k", C.c_int32), ("tokens_dtype", C.c_int32), ("rows_dtype", C.c_int32),
                 ("scale_dtype", C.c_int32), ("mem_axis", C.c_int32), ("tokens", axe_layout_t), ("rows", axe_layout_t),
                 ("tokens_elems", C.c_int64), ("rows_elems", C.c_int64)]
+
+
+class axe_cache_desc_t(C.Structure):
+    _fields_ = [("T", C.c_int64), ("pages", C.c_int64), ("S", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_tokens", C.c_int32), ("max_pages", C.c_int32), ("dtype", C.c_int32), ("cache_dtype", C.c_int32), ("rotary_dim", C.c_int32), ("rotary_style", C.c_int32),
+                ("causal", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("mem_axis", C.c_int32),
+                ("q", axe_layout_t), ("k", axe_layout_t), ("v", axe_layout_t), ("out", axe_layout_t), ("k_cache", axe_layout_t), ("v_cache", axe_layout_t),
+                ("q_elems", C.c_int64), ("k_elems", C.c_int64), ("v_elems", C.c_int64), ("out_elems", C.c_int64), ("k_cache_elems", C.c_int64), ("v_cache_elems", C.c_int64)]
 
 
 class AxeError(RuntimeError):
@@ -142,6 +152,10 @@ def load(path: str) -> C.CDLL:
         getattr(L, name).argtypes = args
     L.axe_rmsnorm_workspace.restype = L.axe_route_workspace.restype = i64
     L.axe_rmsnorm_workspace.argtypes, L.axe_route_workspace.argtypes = [NP], [RP]
+    CP = C.POINTER(axe_cache_desc_t)
+    L.axe_cache_append.restype = L.axe_cache_attention.restype = C.c_int
+    L.axe_cache_append.argtypes, L.axe_cache_attention.argtypes = [CP] + [vp] * 13, [CP] + [vp] * 10 + [i64, vp]
+    L.axe_cache_attention_workspace.restype, L.axe_cache_attention_workspace.argtypes = i64, [CP]
     P64, P32, sz = C.POINTER(i64), C.POINTER(i32), C.c_size_t
     for name, args in (("axe_layout_span", [LP, P64]), ("axe_layout_canonicalize", [LP, LP, vp, sz]),
                        ("axe_layout_gap_condition", [LP]), ("axe_layout_equal", [LP, LP]),
@@ -598,6 +612,70 @@ def axe_rows_combine_backward(desc: RowsDesc, dtokens, rows, row_of, weights, dr
     if rc:
         _check(rc)
     return drows, dweights
+
+
+# ---- attention over a paged cache
+def _strided(layout: Optional[Layout], shape: Sequence[int], elems: Optional[int], axis: str, dtype: int):
+    """_matrix for operands of more dimensions: contiguous in the order of `shape` unless a layout says otherwise."""
+    dense = layout is None
+    if layout is None:
+        D, step = [], 1
+        for n in reversed(shape):
+            D.insert(0, (max(n, 1), step, axis))
+            step *= max(n, 1)
+        layout = Layout({"D": D})
+    if elems is None:
+        a = layout.axis(axis)
+        elems = layout._o[a] + sum((it.extent - 1) * it.stride for it in layout._d[:layout.c.n_d] if it.axis == a and it.stride > 0) + 1 if all(shape) else 0
+    return layout, elems, _operand(elems, _BYTES.get(dtype, 0), dense)
+
+
+class CacheDesc:
+    """Holder of an axe_cache_desc_t: T new tokens of S sequences over a cache of `pages` pages of page_tokens tokens, max_pages of them in a row of the page table.  Layouts of q, k, v, out
+    (tokens, heads, columns) and of the caches (pages, tokens of a page, heads, columns) default to contiguous ones, cache_dtype to dtype, scale to head_dim ** -0.5."""
+
+    def __init__(self, T: int, S: int, q_heads: int, kv_heads: int, head_dim: int, pages: int, page_tokens: int, max_pages: int, dtype: int, cache_dtype: Optional[int] = None,
+                 rotary_dim: int = 0, rotary_style: int = AXE_ROTATE_HALVES, causal: bool = True, window: int = 0, scale: Optional[float] = None, q: Optional[Layout] = None,
+                 k: Optional[Layout] = None, v: Optional[Layout] = None, out: Optional[Layout] = None, k_cache: Optional[Layout] = None, v_cache: Optional[Layout] = None,
+                 q_elems: Optional[int] = None, k_elems: Optional[int] = None, v_elems: Optional[int] = None, out_elems: Optional[int] = None, k_cache_elems: Optional[int] = None,
+                 v_cache_elems: Optional[int] = None, mem_axis: str = "m"):
+        held = dtype if cache_dtype is None else cache_dtype
+        of_q, of_k, of_cache = (T, q_heads, head_dim), (T, kv_heads, head_dim), (pages, page_tokens, kv_heads, head_dim)
+        m = [_strided(L, shape, n, mem_axis, dt) for L, shape, n, dt in ((q, of_q, q_elems, dtype), (k, of_k, k_elems, dtype), (v, of_k, v_elems, dtype), (out, of_q, out_elems, dtype),
+                                                                        (k_cache, of_cache, k_cache_elems, held), (v_cache, of_cache, v_cache_elems, held))]
+        self.layouts = tuple(L for L, _, _ in m)
+        self.c = axe_cache_desc_t(T, pages, S, q_heads, kv_heads, head_dim, page_tokens, max_pages, dtype, held, rotary_dim, rotary_style, int(bool(causal)), window,
+                                  head_dim ** -0.5 if scale is None else scale, _axis_of(mem_axis, *self.layouts), *[L.c for L in self.layouts], *[n for _, n, _ in m])
+        self.ref = C.byref(self.c)
+        self.elems = tuple(n for _, n, _ in m)
+        self.operands = tuple(o for _, _, o in m)
+        self.table, self.angles, self.scales = S * max_pages, max_pages * page_tokens * rotary_dim, pages * page_tokens * kv_heads
+
+
+def axe_cache_append(desc: CacheDesc, k, v, k_cache, v_cache, seq_rows, lengths, page_table, rotation=None, q=None, q_out=None, k_scales=None, v_scales=None, stream=None):
+    """The new tokens' keys (rotated by their positions) and values into their places in the cache, q rotated into q_out."""
+    o_q, o_k, o_v, o_o, o_kc, o_vc = desc.operands
+    rc = (_lib or lib()).axe_cache_append(desc.ref, _ptr(q, o_q), _ptr(k, o_k), _ptr(v, o_v), _floats(rotation, desc.angles), _ints(seq_rows, desc.c.S + 1), _ints(lengths, desc.c.S),
+                                          _ints(page_table, desc.table), _ptr(q_out, o_o), _ptr(k_cache, o_kc), _ptr(v_cache, o_vc), _floats(k_scales, desc.scales),
+                                          _floats(v_scales, desc.scales), _stream_ptr(stream))
+    if rc:
+        _check(rc)
+    return k_cache, v_cache
+
+
+def axe_cache_attention_workspace(desc: CacheDesc) -> int:
+    """4-byte words of the workspace that axe_cache_attention needs."""
+    return _count(lib().axe_cache_attention_workspace(desc.ref))
+
+
+def axe_cache_attention(desc: CacheDesc, q, k_cache, v_cache, seq_rows, lengths, page_table, out, k_scales=None, v_scales=None, workspace=None, stream=None):
+    """Attention of the new tokens' queries over what the cache holds of their sequences."""
+    o_q, _, _, o_o, o_kc, o_vc = desc.operands
+    rc = (_lib or lib()).axe_cache_attention(desc.ref, _ptr(q, o_q), _ptr(k_cache, o_kc), _ptr(v_cache, o_vc), _floats(k_scales, desc.scales), _floats(v_scales, desc.scales),
+                                             _ints(seq_rows, desc.c.S + 1), _ints(lengths, desc.c.S), _ints(page_table, desc.table), _ptr(out, o_o), *_words(workspace), _stream_ptr(stream))
+    if rc:
+        _check(rc)
+    return out
 
 
 def _words(workspace):

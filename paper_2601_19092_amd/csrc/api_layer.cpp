@@ -1,78 +1,13 @@
 // Entry points of what stands around the experts' products: norm, routing, rows in the experts' order.  Argument checks and launches.
 #include <hip/hip_runtime.h>
 
-#include <initializer_list>
-#include <new>
-
-#include "../../include/axe.h"
-#include "host_layout.h"
+#include "entry_points.h"
 #include "layer_ops.h"
 #include "layer_shapes.h"
-#include "plans.h"
 
 using namespace axe;
 
 namespace {
-
-bool real_type(int t) { return t == AXE_BF16 || t == AXE_F16 || t == AXE_F32; }
-
-int invalid(const char* fn, const char* what) {
-  set_error("%s: %s", fn, what);
-  return AXE_EINVAL;
-}
-int unsupported(const char* fn, const char* what) {
-  set_error("%s: %s", fn, what);
-  return AXE_EUNSUPPORTED;
-}
-
-// A buffer of a call: where, how many bytes, what it has to be aligned to, and whether the call may not do without it.
-struct Buf {
-  const void* p;
-  int64_t bytes;
-  int align;
-  bool needed;
-};
-bool meet(const Buf& a, const Buf& b) {
-  return a.p && b.p && (const char*)a.p < (const char*)b.p + b.bytes && (const char*)b.p < (const char*)a.p + a.bytes;
-}
-int check_buffers(const char* fn, std::initializer_list<Buf> in, std::initializer_list<Buf> out) {
-  for (const auto& list : {in, out})
-    for (const Buf& b : list) {
-      if (b.needed && !b.p) return invalid(fn, "NULL device pointer");
-      if (b.p && (uintptr_t)b.p % (uintptr_t)b.align) return invalid(fn, "a buffer is not aligned to its elements");
-    }
-  for (const Buf& o : out) {
-    for (const Buf& i : in)
-      if (meet(i, o)) return invalid(fn, "an output overlaps an input");
-    for (const Buf& p : out)
-      if (&p != &o && meet(p, o)) return invalid(fn, "two outputs overlap");
-  }
-  return AXE_OK;
-}
-
-// One matrix of a call: its layout on the memory axis, planned once per descriptor.  Bytes of its buffer are computed of a matrix that was planned (or is not there) only: 64 bits hold them.
-struct Mat {
-  int64_t ld = 0, off = 0;
-};
-constexpr int64_t kMostElems = int64_t(1) << 58;
-int plan_matrix(const axe_layout_t& L, int mem_axis, int64_t rows, int64_t cols, int64_t elems, const char* fn, Mat& m) {
-  if (elems > kMostElems) return invalid(fn, "a buffer of more than 2^58 elements");
-  return strided_2d(&L, mem_axis, rows, cols, true, elems, fn, &m.ld, &m.off);
-}
-int64_t bytes_of(const void* p, int64_t elems, int eb) { return p ? elems * eb : 0; }
-
-// The body of an entry point; planning allocates, and an entry point neither throws nor aborts.
-template <class F>
-auto guarded(const char* fn, F&& f) -> decltype(f()) {
-  try {
-    return f();
-  } catch (const std::bad_alloc&) {
-    set_error("%s: out of host memory", fn);
-    return AXE_EINVAL;
-  }
-}
-
-int finish(hipError_t e, const char* fn) { return e == hipSuccess ? AXE_OK : hip_fail(e, fn); }
 
 // ---- norm -----------------------------------------------------------------------------------------------------------
 
@@ -113,11 +48,6 @@ int kept_norm_plan(const axe_rmsnorm_desc_t* g, const char* fn, bool res, bool s
   if (int rc = plan_norm(g, fn, res, sum, out)) return rc;
   if (keyed) last.keep(key, out);
   return AXE_OK;
-}
-template <class V>
-V* at(V* p, int64_t off, int eb) {
-  using C = std::conditional_t<std::is_const<V>::value, const char, char>;
-  return p ? (V*)((C*)p + off * eb) : nullptr;
 }
 // an output that is exactly an input: same buffer, same element size, same place of every element
 bool same(const void* a, const Mat& m, int eb, const void* b, const Mat& n, int fb) { return a && a == b && m.ld == n.ld && m.off == n.off && eb == fb; }

@@ -7,6 +7,7 @@
 
 #include <vector>
 
+#include "cache_ops.h"
 #include "device_types.h"
 #include "kernels.h"
 #include "layer_ops.h"
@@ -346,6 +347,8 @@ hipError_t launch_route_backward(const RouteArgs&, hipStream_t) { return hipErro
 hipError_t launch_rows_dispatch(const RowsArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_rows_combine(const RowsArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_rows_combine_backward(const RowsArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_cache_append(const CacheArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_cache_attention(const CacheArgs&, hipStream_t) { return hipErrorNotSupported; }
 
 }  // namespace axe
 

@@ -19,7 +19,7 @@ int strided_2d(const axe_layout_t* L, int mem_axis, int64_t d0, int64_t d1, bool
 // The contents of a descriptor as a flat run of words: what a plan depends on, device pointers aside (of those
 // only whether they are given and their alignment matter).  False when the descriptor is malformed in a way
 // that makes its arrays unreadable: the planner then reports the error.
-constexpr int kKeyWords = 24 + 4 * (12 + 3 * (AXE_MAX_D + AXE_MAX_R) + AXE_MAX_AXES);
+constexpr int kKeyWords = 24 + 6 * (12 + 3 * (AXE_MAX_D + AXE_MAX_R) + AXE_MAX_AXES);   // (six layouts at most)
 struct PlanKey {
   int64_t w[kKeyWords];
   int n = 0;

@@ -1,0 +1,130 @@
+"""Appending keys and values to a paged cache on the GPU against the same in 64 bits.
+
+Tolerances.  U = 2^-24, H = half a step of the 16-bit type relative to the value (2^-8 bf16, 2^-11 fp16).  A turned element is a cos - b sin in fp32, three roundings: 3 U (|a| + |b|); then its own rounding,
+H of the value (fp16: no less than 2^-25).  What is not turned is copied: the same bits.  e4m3: the scale max / 448 is off by that of its largest element and one rounding; a code by half a step
+of e4m3, 2^-4 of the value or half of the smallest step, 2^-10, and by what the element and the scale are off by, in units of the scale."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_ref as R
+from paper_2601_19092_amd import binding as B
+from paper_2601_19092_amd import workloads as W
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+CODE = {"bf16": B.AXE_BF16, "f16": B.AXE_F16, "fp8": B.AXE_FP8_E4M3}
+TORCH = {"bf16": torch.bfloat16, "f16": torch.float16, "fp8": torch.float8_e4m3fn}
+HALF = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float32).double().numpy()
+
+
+def angles(rows, rotary):
+    a = np.arange(rows)[:, None] * 10000.0 ** (-np.arange(0, rotary, 2) / max(rotary, 1))
+    return torch.from_numpy(np.concatenate([np.cos(a), np.sin(a)], 1).astype(np.float32))
+
+
+class Append:
+    """One call: rows of one product (queries, keys and values side by side, pitched), or separate tensors."""
+
+    def __init__(self, lengths, new, Hq, Hkv, D, page, dtype="bf16", cache=None, rotary=None, style="halves", seed=0, shared=True, spare=2, extra_rows=0, std=1.0):
+        g = torch.Generator().manual_seed(seed)
+        cache = cache or dtype
+        rotary = D if rotary is None else rotary
+        S, need = len(lengths), [max(0, -(-n // page)) for n in lengths]
+        self.__dict__.update(lengths=lengths, Hq=Hq, Hkv=Hkv, D=D, page=page, dtype=dtype, cache=cache, style=style, rotary=rotary, pages=sum(need) + spare, most=max(need + [1]))
+        self.table = torch.full((S, self.most), -1, dtype=torch.int32)
+        perm, at = torch.randperm(self.pages, generator=g).int(), 0
+        for s, n in enumerate(need):
+            self.table[s, :n] = perm[at:at + n]
+            at += n
+        self.seq_rows = torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32)
+        T = self.T = int(self.seq_rows[-1]) + extra_rows
+        self.rotation = angles(self.most * page, rotary)
+        pitch = (Hq + 2 * Hkv) * D + 24
+        self.buf = (torch.randn(T * pitch + 40, generator=g) * std).to(TORCH[dtype])
+        view = lambda o, h: torch.as_strided(self.buf, (T, h, D), (pitch, D, 1), o * D + 8)  # noqa: E731
+        self.q, self.k, self.v = view(0, Hq), view(Hq, Hkv), view(Hq + Hkv, Hkv)
+        of = lambda o, h: B.Layout(W.spec([(T, pitch, "m"), (h, D, "m"), (D, 1, "m")], O={"m": o * D + 8}), ["m"])  # noqa: E731
+        kw = dict(q=of(0, Hq), k=of(Hq, Hkv), v=of(Hq + Hkv, Hkv))
+        self.desc = B.CacheDesc(T, S, Hq, Hkv, D, self.pages, page, self.most, CODE[dtype], CODE[cache], rotary_dim=rotary,
+                                rotary_style=B.AXE_ROTATE_PAIRS if style == "pairs" else B.AXE_ROTATE_HALVES, **(kw if shared else {}))
+        self.shared = shared
+
+    def run(self, with_q=True, in_place=False, stream=None):
+        dev = [self.buf.cuda()] * 3 if self.shared else [x.contiguous().cuda() for x in (self.q, self.k, self.v)]
+        shape = (self.pages, self.page, self.Hkv, self.D)
+        kc, vc = (torch.full(shape, 0x55, dtype=torch.uint8, device="cuda") if self.cache == "fp8" else torch.full(shape, 3.0, dtype=TORCH[self.cache], device="cuda") for _ in range(2))
+        sc = [torch.full(shape[:3], 5.0, device="cuda") for _ in range(2)] if self.cache == "fp8" else [None, None]
+        out = torch.full((self.T, self.Hq, self.D), 7.0, dtype=TORCH[self.dtype], device="cuda")
+        held = [c.view(torch.float8_e4m3fn) if self.cache == "fp8" else c for c in (kc, vc)]
+        B.axe_cache_append(self.desc, dev[1], dev[2], held[0], held[1], self.seq_rows.cuda(), torch.tensor(self.lengths, dtype=torch.int32).cuda(), self.table.cuda(),
+                           rotation=self.rotation.cuda() if self.rotary else None, q=dev[0] if with_q else None, q_out=out if with_q else None, k_scales=sc[0], v_scales=sc[1], stream=stream)
+        torch.cuda.synchronize()
+        return out, kc, vc, sc
+
+    def check(self, got, with_q=True):
+        out, kc, vc, sc = got
+        q, k, v = f64(self.q), f64(self.k), f64(self.v)
+        wq, wk, wv = R.append(q, k, v, self.rotation.double().numpy(), self.seq_rows.numpy(), self.lengths, self.table.numpy(), self.page, self.pages, self.style)
+        out = f64(out)
+        for t in range(self.T):
+            if not with_q or t not in wq:
+                assert (out[t] == 7.0).all(), t
+                continue
+            self.near(out[t], wq[t], 3 * U * size(q[t], self.rotary, self.style), ("q", t))
+        for cache, scales, want, of in ((kc, sc[0], wk, k), (vc, sc[1], wv, v)):
+            c = f64(cache.view(torch.float8_e4m3fn) if self.cache == "fp8" else cache)
+            raw = cache.cpu()
+            rows = {at: t for t, s, p in R.tokens(self.seq_rows.numpy(), self.lengths) for at in [R.place(self.table.numpy(), self.page, self.pages, s, p)] if at is not None}
+            for pg in range(self.pages):
+                for sl in range(self.page):
+                    if (pg, sl) not in want:
+                        assert (raw[pg, sl] == (0x55 if self.cache == "fp8" else 3.0)).all(), "places that no token has are left as they are"
+                        assert self.cache != "fp8" or (scales[pg, sl] == 5.0).all()
+                        continue
+                    err = 3 * U * (size(of[rows[pg, sl]], self.rotary, self.style) if of is k else 0.0)
+                    y = want[pg, sl]
+                    if self.cache != "fp8":
+                        self.near(c[pg, sl], y, err, (pg, sl))
+                        continue
+                    s = scales[pg, sl].cpu().double().numpy()
+                    most = np.abs(y).max(1)
+                    s64 = np.where(most > 0, np.maximum(most / 448.0, 2.0 ** -126), 1.0)
+                    assert (np.abs(s - s64) <= s64 * 3 * U + np.max(err) / 448.0).all()
+                    x = np.clip(y / s[:, None], -448, 448)
+                    tol = np.maximum(np.abs(x) * 2.0 ** -4, 2.0 ** -10) + err / s[:, None] + np.abs(x) * 2 * U
+                    assert (np.abs(c[pg, sl] - x) <= tol).all(), (pg, sl)
+        return self
+
+    def near(self, got, want, err, what):
+        tol = np.abs(want) * HALF[self.dtype] + err * (1 + HALF[self.dtype]) + (2.0 ** -25 if self.dtype == "f16" else 0)
+        assert (np.abs(got - want) <= tol).all(), (what, got[np.abs(got - want) > tol][:4], want[np.abs(got - want) > tol][:4])
+
+
+def size(x, rotary, style):
+    """|a| + |b| of every element's pair; 0 where nothing is turned."""
+    y, h = np.zeros_like(x), rotary // 2
+    a, b = (np.arange(h), np.arange(h) + h) if style == "halves" else (2 * np.arange(h), 2 * np.arange(h) + 1)
+    y[:, a] = y[:, b] = np.abs(x[:, a]) + np.abs(x[:, b])
+    return y
+
+
+@pytest.mark.parametrize("dtype, cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "fp8"), ("f16", "fp8")])
+@pytest.mark.parametrize("style", ["halves", "pairs"])
+@pytest.mark.parametrize("D, rotary", [(128, 128), (128, 64), (64, 40), (80, 80), (80, 10), (8, 8), (8, 2), (256, 256), (256, 254), (136, 0)])
+def test_types_columns_rotations(dtype, cache, style, D, rotary):
+    a = Append([70, 3, 33], [20, 3, 1], 4, 2, D, 16, dtype, cache, rotary, style, seed=D + rotary)
+    a.check(a.run())
+
+
+@pytest.mark.parametrize("Hq, Hkv", [(1, 1), (32, 4), (7, 7), (128, 1), (40, 8)])
+def test_heads(Hq, Hkv):
+    for shared in (True, False):
+        a = Append([50, 9], [5, 9], Hq, Hkv, 64, 24, seed=Hq, shared=shared)
+        a.check(a.run())
+        a.check(a.run(with_q=False), with_q=False)
