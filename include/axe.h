@@ -450,10 +450,10 @@ int axe_rows_combine_backward(const axe_rows_desc_t* g, const void* d_dtokens, c
  *
  *   q, k, v, out     : (T, heads, head_dim) of dtype (AXE_BF16 or AXE_F16), any strides of tokens and heads, unit stride along the columns, no replicas; out also stands for the rotated queries.
  *                      T counts the rows; seq_rows are taken as at most T.
- *   k_cache, v_cache : (pages, page_tokens, kv_heads, head_dim) of cache_dtype, dtype or AXE_FP8_E4M3, in any order and with any gaps: unit stride along the columns, the other strides and the offset
- *                      multiples of 8 elements, the address aligned to 8 elements.  e4m3: d_k_scales, d_v_scales (pages, page_tokens, kv_heads) fp32, contiguous; a row of a head is its codes times its scale.
+ *   k_cache, v_cache : (pages, page_tokens, kv_heads, head_dim) of cache_dtype, dtype or AXE_FP8_E4M3, in any order and with any gaps: unit stride along the columns, the other strides, the offset
+ *                      and the address multiples of 16 bytes.  e4m3: d_k_scales, d_v_scales (pages, page_tokens, kv_heads) fp32, contiguous; a row of a head is its codes times its scale.
  *   q_heads          : a multiple of kv_heads, at most 128 times as many; head h reads head h / (q_heads / kv_heads) of the cache.
- *   head_dim         : a multiple of 8 up to 256.  T, max_pages page_tokens and pages up to 2^30, S below 2^20, heads below 2^16.
+ *   head_dim         : a multiple of 8, with an e4m3 cache of 16, up to 256.  T, max_pages page_tokens and pages up to 2^30, S below 2^20, heads below 2^16.
  *
  * axe_cache_append -- cache[s, p] = (rot_p(k), v), q_out = rot_p(q) for every new token.
  *   rot_p turns the first rotary_dim (even, up to head_dim, or 0) columns of a head in pairs, (a, b) -> (a cos - b sin, b cos + a sin): columns (i, i + rotary_dim / 2) (AXE_ROTATE_HALVES) or

@@ -20,7 +20,7 @@ int check_cache(const axe_cache_desc_t* g, const char* fn) {
   if (!real_type(g->dtype) || !(real_type(g->cache_dtype) || g->cache_dtype == AXE_FP8_E4M3)) return invalid(fn, "unknown element type");
   if (g->q_heads % g->kv_heads) return invalid(fn, "q_heads must be a multiple of kv_heads");
   if (g->dtype == AXE_F32 || (g->cache_dtype != g->dtype && g->cache_dtype != AXE_FP8_E4M3)) return unsupported(fn, "rows in bf16 or fp16, the cache in the same or in e4m3");
-  if (g->head_dim % 8 || g->head_dim > 256) return unsupported(fn, "head_dim must be a multiple of 8 up to 256");
+  if (g->head_dim % (g->cache_dtype == AXE_FP8_E4M3 ? 16 : 8) || g->head_dim > 256) return unsupported(fn, "head_dim must be a multiple of 8 (of 16 with an e4m3 cache) up to 256");
   if (g->q_heads / g->kv_heads > kAttnMaxGroup || g->q_heads >= 65536 || g->S >= 1 << 20 || g->T > kMost || g->pages > kMost || (int64_t)g->max_pages * g->page_tokens > kMost)
     return unsupported(fn, "T, pages, max_pages page_tokens up to 2^30, S below 2^20, heads below 2^16, at most 128 query heads to a head of the cache");
   return AXE_OK;
@@ -88,7 +88,8 @@ int plan_cache(const axe_cache_desc_t* g, const char* fn, Uses u, CachePlan& p) 
       set_error("%s: two elements of a cache may share an address", fn);
       return AXE_EALIAS;
     }
-    if (c->s[0] % 8 || c->s[1] % 8 || c->s[2] % 8 || c->off % 8) return unsupported(fn, "a cache's strides and offset must be multiples of 8 elements");
+    const int unit = g->cache_dtype == AXE_FP8_E4M3 ? 16 : 8;
+    if (c->s[0] % unit || c->s[1] % unit || c->s[2] % unit || c->off % unit) return unsupported(fn, "a cache's strides and offset must be multiples of 16 bytes");
   }
   return AXE_OK;
 }
@@ -181,7 +182,7 @@ int axe_cache_append(const axe_cache_desc_t* g, const void* d_q, const void* d_k
     Buf q = {d_q, has_q ? g->q_elems * eb : 0, eb, false}, k = {d_k, g->k_elems * eb, eb, true}, v = {d_v, g->v_elems * eb, eb, true};
     Buf rot = {g->rotary_dim ? d_rotation : nullptr, (int64_t)g->max_pages * g->page_tokens * g->rotary_dim * 4, 4, g->rotary_dim && g->max_pages};
     Buf o = {d_q_out, has_q ? g->out_elems * eb : 0, eb, false};
-    Buf kc = {any ? d_k_cache : nullptr, any ? g->k_cache_elems * cb : 0, 8 * cb, any}, vc = {any ? d_v_cache : nullptr, any ? g->v_cache_elems * cb : 0, 8 * cb, any};
+    Buf kc = {any ? d_k_cache : nullptr, any ? g->k_cache_elems * cb : 0, 16, any}, vc = {any ? d_v_cache : nullptr, any ? g->v_cache_elems * cb : 0, 16, any};
     Buf sk = {any ? d_k_scales : nullptr, fp8 ? cache_scale_bytes(g) : 0, 4, fp8 && any}, sv = {any ? d_v_scales : nullptr, fp8 ? cache_scale_bytes(g) : 0, 4, fp8 && any};
     // q in place: a thread reads the elements that it writes, and those they are turned with, before the wave that holds them writes any
     Buf qi = q, ki = k, vi = v;
@@ -209,7 +210,7 @@ int axe_cache_append(const axe_cache_desc_t* g, const void* d_q, const void* d_k
 int64_t axe_cache_attention_workspace(const axe_cache_desc_t* g) {
   return guarded("axe_cache_attention_workspace", [&]() -> int64_t {
     if (int rc = check_cache(g, "axe_cache_attention_workspace")) return rc;
-    return attn_workspace_words(g->T, g->S, g->kv_heads, g->q_heads / g->kv_heads, g->head_dim);
+    return attn_workspace_words(attn_shape(g->T, g->S, g->kv_heads, g->q_heads / g->kv_heads, g->head_dim), g->head_dim);
   });
 }
 
@@ -228,11 +229,12 @@ int axe_cache_attention(const axe_cache_desc_t* g, const void* d_q, const void* 
     if (int rc = kept_cache_plan(g, fn, {true, false, true}, kept)) return rc;
     const CachePlan& p = *kept;
     const int G = g->q_heads / g->kv_heads, eb = 2, cb = fp8 ? 1 : 2;
-    const int64_t words = attn_workspace_words(g->T, g->S, g->kv_heads, G, g->head_dim);
+    const AttnShape shape = attn_shape(g->T, g->S, g->kv_heads, G, g->head_dim);
+    const int64_t words = attn_workspace_words(shape, g->head_dim);
     if (words > 0 && (!d_ws || ws_elems < words)) return invalid(fn, "the workspace is smaller than axe_cache_attention_workspace");
     const Tables t = tables(g, d_seq_rows, d_lengths, d_page_table);
-    if (int rc = check_buffers(fn, {{d_q, g->q_elems * eb, eb, true}, {any ? d_k_cache : nullptr, any ? g->k_cache_elems * cb : 0, 8 * cb, any},
-                                    {any ? d_v_cache : nullptr, any ? g->v_cache_elems * cb : 0, 8 * cb, any}, {any ? d_k_scales : nullptr, fp8 ? cache_scale_bytes(g) : 0, 4, fp8 && any},
+    if (int rc = check_buffers(fn, {{d_q, g->q_elems * eb, eb, true}, {any ? d_k_cache : nullptr, any ? g->k_cache_elems * cb : 0, 16, any},
+                                    {any ? d_v_cache : nullptr, any ? g->v_cache_elems * cb : 0, 16, any}, {any ? d_k_scales : nullptr, fp8 ? cache_scale_bytes(g) : 0, 4, fp8 && any},
                                     {any ? d_v_scales : nullptr, fp8 ? cache_scale_bytes(g) : 0, 4, fp8 && any}, t.rows, t.lengths, t.pages},
                                {{d_out, g->out_elems * eb, eb, true}, {words ? d_ws : nullptr, words * 4, 16, false}}))
       return rc;
@@ -242,7 +244,8 @@ int axe_cache_attention(const axe_cache_desc_t* g, const void* d_q, const void* 
     a.seq_rows = d_seq_rows, a.lengths = d_lengths, a.table = d_page_table, a.ws = (float*)d_ws;
     a.causal = g->causal != 0, a.window = std::min<int64_t>(g->window, kMost);
     a.scale_log2 = (float)(g->scale * 1.4426950408889634);
-    a.groups = words ? attn_slots(g->head_dim) : 0, a.ws_rows = attn_ws_rows(g->T, G);
+    a.sixteens = g->page_tokens % 16 == 0 && std::max(p.kc.s[1], p.vc.s[1]) < (int64_t(1) << 26);
+    a.groups = shape.groups, a.tile_rows = shape.tile_rows, a.ws_rows = shape.ws_rows;
     return finish(launch_cache_attention(a, (hipStream_t)stream), fn);
   });
 }

@@ -1,0 +1,970 @@
+// Attention of new tokens over a paged cache (axe_cache_attention): the kernels.  Device code, gfx950 only.
+//
+//   o[t, h] = sum_j softmax_j(scale q[t, h] . K[j]) V[j]
+//
+// A tile is 128 rows: the query heads of one head of the cache, of consecutive new tokens of one sequence (row r: token r / G, head r mod G), so that one pass over the keys
+// serves all of them.  A workgroup of four waves takes a tile's keys 64 at a time: K and V of the 64 go straight from their pages to LDS (two blocks of LDS, one filled while the
+// other is read), and every wave has 32 rows for itself:
+//   S^T = K Q^T      a lane holds 32 of the 64 scores of one row, lane + 32 the others: maximum and sum of a row are a chain in the lane and one exchange;
+//   O^T += V^T P^T   the scores' registers, in 16 bits, are the product's operand as they are: its contraction runs over the keys in the order in which the registers hold them, and V comes out of LDS in
+//                    that order by transposing reads.
+// The maximum is a running one: when it grows, sums and O are multiplied down.  Everything but the products' operands is fp32.
+//
+// Where a batch has few tiles, the list of all (tile, block of keys) is cut into as many equal runs as there are workgroups, wherever that falls; a tile that is cut leaves partial
+// results (maximum, sum, O) in the workspace, and a second kernel joins them, in the order of the keys.  Which run a workgroup has follows from the lengths alone: results repeat
+// their bits.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "cache_ops.h"
+#include "cache_tables.h"
+#include "gemm_common.h"
+#include "row_ops.h"
+
+namespace axe {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+typedef __attribute__((address_space(3))) s16x4* tr_ptr;
+typedef __attribute__((address_space(3))) i32x2* tr8_ptr;
+
+template <int TYPE>
+__device__ __forceinline__ f32x16 mfma32(s16x8 a, s16x8 b, f32x16 c) {
+  if constexpr (TYPE == kBf16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if constexpr (TYPE == kBf16) return pack_bf16(lo, hi);
+  else {
+    typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+    return __builtin_bit_cast(uint32_t, f16x2{(_Float16)lo, (_Float16)hi});
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
+  if constexpr (TYPE == kBf16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <int TYPE>
+__device__ __forceinline__ f32x4 mfma16_short(s16x4 a, s16x4 b, f32x4 c) {
+  typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+  if constexpr (TYPE == kBf16) return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, a), __builtin_bit_cast(f16x4, b), c, 0, 0, 0);
+}
+// Eight e4m3 numbers in 16 bits, which hold them all.
+template <int TYPE>
+__device__ __forceinline__ s16x8 widen(u32x2 v) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (TYPE == kBf16) {
+      r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], 1.0f, false));
+      r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], 1.0f, true));
+    } else {
+      r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[i], 1.0f, false));
+      r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[i], 1.0f, true));
+    }
+  }
+  return __builtin_bit_cast(s16x8, r);
+}
+template <int TYPE>
+__device__ __forceinline__ float half(uint32_t two, int which) {
+  if constexpr (TYPE == kBf16) return __uint_as_float(which ? two & 0xffff0000u : two << 16);
+  else return (float)__builtin_bit_cast(_Float16, (uint16_t)(two >> which * 16));
+}
+// What a term p counts in the sum when the product with V has t = p v, v the scale of V's row, as `rounded`: rounded / v.  A key that has nearly all the weight then has V's row for its result, not that times
+// the error of one rounding.
+__device__ __forceinline__ float weight(float p, float t, float v, float rounded) {
+  const float by = __builtin_amdgcn_rcpf(v);
+  return fabsf(v) >= 1e-30f && fabsf(v) <= 1e30f ? fmaf(rounded - t, by, p) : p;
+}
+// v of the four lanes of a column (lane mod 16) joined.
+template <class OP>
+__device__ __forceinline__ float quarters(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+  v = OP::of(__int_as_float(a[0]), __int_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+  return OP::of(__int_as_float(b[0]), __int_as_float(b[1]));
+}
+__device__ __forceinline__ float other_half(float v) {              // of lane ^ 32
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+  return __int_as_float((threadIdx.x & 32) ? s[0] : s[1]);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// 16 bytes that are zero: what a lane brings to LDS for a key that is not there.
+__device__ const u32x4 kNothing = {0, 0, 0, 0};
+
+// Loads into LDS, 16 bytes a lane: the wave's 1024 bytes from `lds` on.  (Written as asm: the compiler would wait for them before it reads any of LDS.  M0 holds the address;
+// the wait states are for registers that a vector instruction may just have written.)
+__device__ __forceinline__ void load_lds(const void* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void load_lds(uint32_t offset, const void* base, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
+}
+
+// The same, 4 bytes a lane.
+__device__ __forceinline__ void load_lds4(const void* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(lds) : "memory");
+}
+
+// ---- the batch
+
+struct Seq {
+  int row0, n;                     // its rows
+  int first;                       // position of its first new token
+  int len;                         // keys
+};
+__device__ __forceinline__ Seq sequence(const CacheArgs& a, int s) {
+  const int T = (int)a.T, b0 = a.seq_rows[s], b1 = a.seq_rows[s + 1], l = a.lengths[s];
+  Seq q;
+  q.row0 = b0 < 0 ? 0 : b0 > T ? T : b0;
+  const int end = b1 > T ? T : b1;
+  q.n = end > q.row0 ? end - q.row0 : 0;
+  const int length = l < 0 ? 0 : l;
+  q.len = length < a.capacity ? length : a.capacity;
+  q.first = length - q.n;
+  return q;
+}
+// Keys that tokens i0 .. i1 of a sequence see between them, [lo, hi).
+struct Range {
+  int lo, hi;
+};
+__device__ __forceinline__ Range seen(const CacheArgs& a, const Seq& q, int i0, int i1) {
+  Range r = {0, q.len};
+  if (a.causal) {
+    const int end = q.first + i1 + 1;
+    r.hi = end < r.hi ? (end > 0 ? end : 0) : r.hi;
+    if (a.window) {
+      const int at = q.first + i0 + 1 - a.window;
+      r.lo = at < 0 ? 0 : at < a.capacity ? at : a.capacity;
+    }
+  }
+  return r;
+}
+struct Blocks {
+  int first, count;                // a tile without keys has one block, without keys
+};
+__device__ __forceinline__ Blocks blocks_of(const Range& r) {
+  const int first = r.lo / kAttnKeys, end = (r.hi + kAttnKeys - 1) / kAttnKeys;
+  return Blocks{first, end > first ? end - first : 1};
+}
+__device__ __forceinline__ int tiles_of(const CacheArgs& a, const Seq& q, int tokens) { return (q.n + tokens - 1) / tokens; }
+__device__ __forceinline__ Blocks tile_blocks(const CacheArgs& a, const Seq& q, int tokens, int tile) {
+  const int i0 = tile * tokens, i1 = (i0 + tokens < q.n ? i0 + tokens : q.n) - 1;
+  return blocks_of(seen(a, q, i0, i1));
+}
+// The split form takes a sequence's tiles in pairs, the first with the last: they have about the same number of blocks together, at most `cell`, which is what a pair counts.
+struct Cost {
+  int pairs, cell;
+};
+__device__ __forceinline__ Cost cost_of(const CacheArgs& a, const Seq& q, int tokens) {
+  const int tiles = tiles_of(a, q, tokens);
+  if (tiles <= 1) return Cost{tiles, tiles ? tile_blocks(a, q, tokens, 0).count : 0};
+  int64_t cell = 2 * (int64_t)((q.len + kAttnKeys - 1) / kAttnKeys);
+  if (a.causal) {
+    const int64_t up = (2 * (int64_t)(q.first > 0 ? q.first : 0) + (int64_t)(tiles + 1) * tokens + 2 * (kAttnKeys - 1)) / kAttnKeys;
+    cell = up < cell ? up : cell;
+    if (a.window) {
+      const int64_t w = 2 * (((int64_t)a.window + tokens) / kAttnKeys + 2);
+      cell = w < cell ? w : cell;
+    }
+  }
+  return Cost{(tiles + 1) / 2, (int)(cell > 2 ? cell : 2)};
+}
+
+// What a workgroup works on: a tile, or a run of its blocks.
+struct Item {
+  Seq q;
+  int s, head;                     // sequence, head of the cache
+  int i0, tokens;                  // its tokens
+  Range keys;
+  int b0, b1;                      // blocks of keys
+};
+
+// Offset of a partial result in the workspace, words.
+__device__ __forceinline__ int64_t part_at(const CacheArgs& a, int group, int which, int DP) { return ((int64_t)group * 2 + which) * (4 + 2 * (int64_t)a.ws_rows + (int64_t)a.ws_rows * DP); }
+
+// ---- the kernel
+
+// RT 0: wide tiles of 128 rows; 1, 2: narrow ones of 16 RT rows.
+template <int TYPE, bool FP8, int DP, int RT>
+struct Attention {
+  static constexpr int ROWS = RT ? 16 * RT : kAttnRows;
+  static constexpr int ROW = DP * 2;                               // bytes of a key in LDS, in 16 bits
+  static constexpr int BLOCK = kAttnKeys * ROW;                    // of K, or V, of a block
+  static constexpr int STEPS = DP / 16, DT = DP / 32;
+  // exp2 of this is a factor of the softmax's terms: fp16 has few numbers below 1
+  static constexpr float LIFT = TYPE == kBf16 ? 0.0f : FP8 ? 8.0f : 15.0f;
+
+  // Sixteen keys as loads of 16 bytes a lane bring them to LDS: CH chunks a key, RPI keys a load, NI loads.  Chunks change places by the key's number, so that what is read
+  // together lies in different banks.
+  template <int EB>
+  struct Sixteen {
+    static constexpr int CH = DP * EB / 16, RPI = 64 / CH, NI = 16 / RPI;
+    static __device__ __forceinline__ int place(bool v, int row) { return EB == 1 ? (CH >= 8 ? row & 7 : row >> 1 & 3) : v ? (row & 3) << 1 : row & 7; }
+  };
+  using S2 = Sixteen<2>;
+  using SN = Sixteen<FP8 ? 1 : 2>;
+
+  // Narrow tiles: a wave has keys for itself, KT at a time, and LDS of its own for two such turns.
+  static constexpr int KT = FP8 ? 32 : 16, NROW = FP8 ? DP : ROW, TURN = KT * NROW;
+
+  struct Shared {
+    union {
+      __attribute__((aligned(16))) uint8_t kv[2][2][BLOCK];        // wide: [stage][K, V]
+      __attribute__((aligned(16))) uint8_t own[4][2][2][TURN];     // narrow: [wave][turn][K, V]
+    };
+    float scales[2][2][2 * kAttnKeys];                             // wide: [stage][K, V] of 64 keys; narrow: [wave][turn] of 32 keys, K then V
+    float top[4][32], sum[4][32];                                  // narrow: the waves' maxima and sums
+    uint16_t there[2][4];                                          // wide: of a wave's 16 keys: which there are
+    int flags[4];
+    int64_t sums[8];
+    int64_t found[4];
+  };
+  static_assert(4 * 2 * 2 * TURN <= 2 * 2 * BLOCK && sizeof(Shared::scales) == 4 * 2 * 64 * 4, "a turn of all waves is no more than a stage");
+
+  const CacheArgs& a;
+  Shared& sh;
+  const int lane, wave, h;
+  Item it;
+
+  // 64 entries of the sequence's page table, a lane each, from page `page0` on
+  int entries, page0;
+
+  __device__ __forceinline__ Attention(const CacheArgs& a_, Shared& s_) : a(a_), sh(s_), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), h((threadIdx.x >> 5) & 1) {}
+
+  static __device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)p); }
+
+  // ---- keys from their pages
+
+  __device__ __forceinline__ void need_pages(int first, int count) {   // of keys first .. first + count - 1, at most 32
+    const int from = first > it.keys.lo ? first : it.keys.lo, end = first + count < it.keys.hi ? first + count : it.keys.hi;
+    if (from >= end) return;
+    const int p0 = (int)quotient(from, a.page), p1 = (int)quotient(end - 1, a.page);
+    if (p1 - page0 < 64 && p0 >= page0) return;
+    page0 = p0;
+    entries = p0 + lane < a.max_pages ? a.table[(int64_t)it.s * a.max_pages + p0 + lane] : -1;
+    asm volatile("" : "+v"(entries));                              // (waited for here, where it is rare: the loads into LDS would be waited for too)
+  }
+  // Whether sixteen keys from `first`, a multiple of 16, on all are there, side by side in one page; then where they begin.
+  __device__ __forceinline__ bool together(int first, int& page, int& slot) {
+    if (!a.sixteens || first < it.keys.lo || first + 16 > it.keys.hi) return false;
+    const int p = (int)quotient(first, a.page);
+    page = __builtin_amdgcn_readlane(entries, p - page0);
+    slot = first - p * (int)a.page.d;
+    return (uint32_t)page < (uint64_t)a.pages;
+  }
+  // Where a lane's key lies; false: it is not there.  (All lanes take part.)
+  __device__ __forceinline__ bool where(int key, int& page, int& slot) {
+    const bool in = key >= it.keys.lo && key < it.keys.hi;
+    const int p = in ? (int)quotient(key, a.page) : page0;
+    page = __shfl(entries, (p - page0) & 63);
+    slot = in ? key - p * (int)a.page.d : 0;
+    return in && (uint32_t)page < (uint64_t)a.pages;
+  }
+  // Sixteen keys (K or V) to LDS.  Returns which there are.
+  template <int EB>
+  __device__ __forceinline__ uint32_t bring(bool v, int first, uint32_t lds) {
+    using S = Sixteen<EB>;
+    const CachePlaces& pl = v ? a.vp : a.kp;
+    const uint8_t* cache = (const uint8_t*)(v ? a.v_cache : a.k_cache) + (int64_t)it.head * pl.head * EB;
+    int page, slot;
+    if (together(first, page, slot)) {
+      const uint8_t* base = cache + (page * pl.page + slot * pl.slot) * EB;
+#pragma unroll
+      for (int i = 0; i < S::NI; ++i) {
+        const int row = i * S::RPI + lane / S::CH, c = (lane % S::CH ^ S::place(v, row)) * 16;
+        const uint32_t off = (uint32_t)(row * (int)pl.slot * EB + c);
+        if (DP == 128 || c < a.D * EB) load_lds(off, base, lds + i * 1024);   // (the others' places hold zeros, see clear_lds)
+      }
+      return 0xffff;
+    }
+    uint32_t there = 0;
+#pragma unroll
+    for (int i = 0; i < S::NI; ++i) {
+      const int row = i * S::RPI + lane / S::CH, c = (lane % S::CH ^ S::place(v, row)) * 16;
+      const bool on = where(first + row, page, slot);
+      const uint8_t* from = cache + (page * pl.page + slot * pl.slot) * EB + c;
+      load_lds(on && c < a.D * EB ? (const void*)from : (const void*)&kNothing, lds + i * 1024);
+      there |= on ? 1u << row : 0u;
+    }
+    return wave_or(there);
+  }
+  static __device__ __forceinline__ uint32_t wave_or(uint32_t v) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v |= (uint32_t)__shfl_xor((int)v, d);
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+  }
+  // Columns from D to DP stay zero: nothing is loaded there.
+  __device__ __forceinline__ void clear_lds() {
+    if (a.D == DP) return;
+    for (int i = threadIdx.x; i < (int)sizeof(sh.kv) / 16; i += 256) ((u32x4*)&sh.kv[0][0][0])[i] = u32x4{};
+    lds_barrier();
+  }
+
+  // ---- wide tiles
+
+  s16x8 q[RT ? 1 : STEPS];
+  f32x16 o[RT ? 1 : DT];
+  float m, l;                                                      // running maximum (scaled) and this lane's part of the sum
+  int lo, hi;                                                      // keys that this lane's row sees
+  int w_lo, w_hi_all, w_lo_all, w_hi;                              // of the wave's rows: seen by any, by all
+  bool rows_here;
+  float lift_v;                                                    // e4m3 values in fp16: what their scales are divided by, a power of two
+  u32x2 kreg[FP8 ? S2::NI : 1], vreg[FP8 ? S2::NI : 1];            // e4m3: a block on its way
+  float sreg[2];
+
+  // Starts the loads of a wave's keys of a block into a stage (e4m3: into registers).
+  __device__ __forceinline__ void issue(int block, int stage) {
+    const int first = block * kAttnKeys + wave * 16;
+    need_pages(first, 16);
+    uint32_t there = 0;
+    if constexpr (!FP8) {
+      there = bring<2>(false, first, lds_at(&sh.kv[stage][0][wave * 16 * ROW]));
+      bring<2>(true, first, lds_at(&sh.kv[stage][1][wave * 16 * ROW]));
+    } else {
+      int page, slot;
+#pragma unroll
+      for (int i = 0; i < S2::NI; ++i) {
+        const int row = i * S2::RPI + lane / S2::CH, kc = (lane % S2::CH ^ S2::place(false, row)) * 8, vc = (lane % S2::CH ^ S2::place(true, row)) * 8;
+        const bool on = where(first + row, page, slot);
+        there |= on ? 1u << row : 0u;
+        const int64_t kat = page * a.kp.page + slot * a.kp.slot + it.head * a.kp.head, vat = page * a.vp.page + slot * a.vp.slot + it.head * a.vp.head;
+        kreg[i] = vreg[i] = u32x2{};
+        if (on && kc < a.D) kreg[i] = *(const u32x2*)((const uint8_t*)a.k_cache + kat + kc);
+        if (on && vc < a.D) vreg[i] = *(const u32x2*)((const uint8_t*)a.v_cache + vat + vc);
+      }
+      const bool on = where(first + (lane & 15), page, slot);      // lane i brings the scales of key i
+      sreg[0] = sreg[1] = 0;
+      if (on) {
+        const int64_t at = ((int64_t)page * a.page.d + slot) * a.kv_heads + it.head;
+        sreg[0] = a.k_scales[at], sreg[1] = a.v_scales[at];
+      }
+      there = wave_or(there);
+    }
+    if (lane == 0) sh.there[stage][wave] = (uint16_t)there;
+  }
+  // e4m3: the block in registers becomes 16 bits in LDS.
+  __device__ __forceinline__ void settle(int stage) {
+    if constexpr (FP8) {
+#pragma unroll
+      for (int i = 0; i < S2::NI; ++i) {
+        const uint32_t at = (wave * 16 + i * S2::RPI) * ROW + lane * 16;
+        *(s16x8*)&sh.kv[stage][0][at] = widen<TYPE>(kreg[i]);
+        *(s16x8*)&sh.kv[stage][1][at] = widen<TYPE>(vreg[i]);
+      }
+      if (lane < 16) sh.scales[stage][0][wave * 16 + lane] = sreg[0], sh.scales[stage][1][wave * 16 + lane] = sreg[1];
+    }
+  }
+
+  __device__ __forceinline__ void begin() {
+    const int G = a.group.d;
+    const int r = wave * 32 + (lane & 31), rows = it.tokens * G;
+    const bool on = r < rows;
+    rows_here = wave * 32 < rows;
+    const int rr = on ? r : rows - 1, i = (int)quotient(rr, a.group), g = rr - i * G;
+    const uint16_t* from = (const uint16_t*)a.q + (int64_t)(it.q.row0 + it.i0 + i) * a.qs.token + (int64_t)(it.head * G + g) * a.qs.head;
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+      const int c = k * 16 + h * 8;
+      q[k] = s16x8{};
+      if (on && c < a.D) q[k] = __builtin_bit_cast(s16x8, load_bits<u32x4>(from + c));
+    }
+    const Range mine = seen(a, it.q, it.i0 + i, it.i0 + i);
+    lo = mine.lo, hi = mine.hi;
+    const int last = rows - 1 < wave * 32 + 31 ? rows - 1 : wave * 32 + 31;
+    const Range f = seen(a, it.q, it.i0 + (int)quotient(rows_here ? wave * 32 : 0, a.group), it.i0 + (int)quotient(rows_here ? wave * 32 : 0, a.group));
+    const Range b = seen(a, it.q, it.i0 + (int)quotient(last, a.group), it.i0 + (int)quotient(last, a.group));
+    w_lo = f.lo, w_lo_all = b.lo, w_hi_all = f.hi, w_hi = b.hi;    // (both ends grow with the token)
+    m = -INFINITY, l = 0, lift_v = 1;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] = f32x16{};
+  }
+
+  // A block's share of the wave's rows, from a stage.
+  __device__ __forceinline__ void compute(int block, int stage) {
+    const int k0 = block * kAttnKeys;
+    if (!rows_here || k0 >= w_hi || k0 + kAttnKeys <= w_lo) return;
+    const uint64_t there = *(const uint64_t*)&sh.there[stage][0];
+    const uint32_t t0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)there), t1 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(there >> 32));
+    const bool masked = (t0 & t1) != 0xffffffffu || k0 < w_lo_all || k0 + kAttnKeys > w_hi_all;
+    const uint8_t *K = sh.kv[stage][0], *V = sh.kv[stage][1];
+    f32x16 s[2] = {f32x16{}, f32x16{}};
+    {
+      const uint32_t at = (lane & 31) * ROW + (h ^ S2::place(false, lane & 31)) * 16;
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) s[t] = mfma32<TYPE>(*(const s16x8*)(K + ((at ^ (k * 32)) + t * 32 * ROW)), q[k], s[t]);
+      }
+    }
+    if constexpr (FP8) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x4 sc = *(const f32x4*)&sh.scales[stage][0][t * 32 + r * 8 + h * 4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t][r * 4 + e] *= sc[e];
+        }
+    }
+    if (masked) {
+      const uint32_t mine[2] = {t0 >> (h * 4), t1 >> (h * 4)};
+      const int low = lo - k0 - h * 4;
+      const uint32_t many = hi > lo ? hi - lo : 0;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int k = (r >> 2) * 8 + (r & 3);
+          s[t][r] = (uint32_t)(t * 32 + k - low) < many && (mine[t] & 1u << k) ? s[t][r] : -INFINITY;
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int r = 1; r < 32; ++r) top = fmaxf(top, s[r >> 4][r & 15]);
+    top = fmaxf(top, other_half(top)) * a.scale_log2;
+    const float grown = fmaxf(m, top);
+    if (__any(grown > m)) {
+      const float by = grown > m ? exp2_fast(m - grown) : 1.0f;    // (the first time: m is -inf, the sums are 0)
+      m = grown, l *= by;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] *= by;
+    }
+    const float less = LIFT - (m == -INFINITY ? 0.0f : m);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[t][r] = exp2_fast(fmaf(s[t][r], a.scale_log2, less));
+        if constexpr (!FP8) l += s[t][r];
+      }
+    float by_v = 1;
+    if constexpr (FP8 && TYPE == kF16) {                           // as in run_narrow
+      const float sv = sh.scales[stage][1][lane], most = wave_all<Max>(fabsf(sv) <= 3.0e38f ? fabsf(sv) : 0.0f);
+      if (most > lift_v) {
+        const float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + 0x800000u), down = lift_v / to;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[t][r] *= down;
+        lift_v = to;
+      }
+      by_v = 1.0f / lift_v;
+    }
+    s16x8 p[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = (k & 1) * 8 + 2 * e;
+        const float x = s[k >> 1][r], y = s[k >> 1][r + 1];
+        if constexpr (FP8) {
+          const float* sc = &sh.scales[stage][1][k * 16 + (e >> 1) * 8 + h * 4 + (e & 1) * 2];
+          const float v0 = sc[0] * by_v, v1 = sc[1] * by_v, t0 = x * v0, t1 = y * v1;
+          w[e] = pack2<TYPE>(t0, t1);
+          l += weight(x, t0, v0, half<TYPE>(w[e], 0)) + weight(y, t1, v1, half<TYPE>(w[e], 1));
+        } else w[e] = pack2<TYPE>(x, y);
+      }
+      p[k] = __builtin_bit_cast(s16x8, w);
+    }
+    // lane i of 16 points at 4 columns of key i / 4 and receives 4 keys of column i
+    const int i = lane & 15, row = h * 4 + (i >> 2);
+    const uint32_t at = row * ROW + ((((lane >> 4) & 1) * 2 + ((i & 3) >> 1)) ^ S2::place(true, row)) * 16 + (i & 1) * 8;
+    auto values = [&](int t, int k) __attribute__((always_inline)) {
+      const uint8_t* v0 = V + ((at ^ (t * 64)) + k * 16 * ROW);
+      const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)v0), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(v0 + 8 * ROW));
+      return s16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    };
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[t] = mfma32<TYPE>(values(t, k), p[k], o[t]);
+  }
+
+  // All blocks of the item, for the rows of all waves.
+  __device__ __forceinline__ void run_wide() {
+    begin();
+    clear_lds();
+    issue(it.b0, 0);
+    for (int b = it.b0; b < it.b1; ++b) {
+      const int stage = (b - it.b0) & 1;
+      settle(stage);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      lds_barrier();
+      if (b + 1 < it.b1) issue(b + 1, stage ^ 1);
+      compute(b, stage);
+    }
+    l += other_half(l);
+    if constexpr (FP8 && TYPE == kF16) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] *= lift_v;
+    }
+  }
+  // Whether x, 0 as long as all results are finite, is anything else in a thread of the workgroup.
+  __device__ __forceinline__ bool not_finite(float x) {
+    const bool any = __any(!(x == 0.0f));
+    if (lane == 0) sh.flags[wave] = any;
+    lds_barrier();
+    return (sh.flags[0] | sh.flags[1] | sh.flags[2] | sh.flags[3]) != 0;
+  }
+  __device__ __forceinline__ float check_wide() {
+    float x = 0;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x = fmaf(o[t][r], 0.0f, x);
+    return x;
+  }
+
+  // The item's result: part < 0: to out; else a partial result, of which these are the tokens from `skip` on.
+  __device__ __forceinline__ void finish_wide(int group, int part, int ends, int skip, int of) {
+    const int G = a.group.d, r = wave * 32 + (lane & 31), rows = it.tokens * G;
+    const bool on = r < rows;
+    if (part < 0) {
+      const float by = l == 0 ? 0.0f : 1.0f / l;
+      const int i = (int)quotient(on ? r : 0, a.group), g = (on ? r : 0) - i * G;
+      uint16_t* to = (uint16_t*)a.out + (int64_t)(it.q.row0 + it.i0 + i) * a.os.token + (int64_t)(it.head * G + g) * a.os.head;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int c = 0; c < 4; c += 2) {                           // the two halves of a lane pair hold columns 4 h .. of chunks c and c + 1: they swap, and each has a chunk
+          const f32x16& v = o[t];
+          const auto x = __builtin_amdgcn_permlane32_swap(pack2<TYPE>(v[c * 4] * by, v[c * 4 + 1] * by), pack2<TYPE>(v[c * 4 + 4] * by, v[c * 4 + 5] * by), false, false);
+          const auto y = __builtin_amdgcn_permlane32_swap(pack2<TYPE>(v[c * 4 + 2] * by, v[c * 4 + 3] * by), pack2<TYPE>(v[c * 4 + 6] * by, v[c * 4 + 7] * by), false, false);
+          const int col = t * 32 + (c + h) * 8;
+          if (on && col < a.D) store_bits(to + col, u32x4{(uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]});
+        }
+      return;
+    }
+    float* p = a.ws + part_at(a, group, part, DP);
+    if (threadIdx.x == 0) *(u32x4*)p = u32x4{(uint32_t)(1 | ends << 1), (uint32_t)(it.q.row0 + it.i0 - skip), (uint32_t)it.head, (uint32_t)(of * G)};
+    if (on) {
+      const int at = skip * G + r;
+      if (h == 0) p[4 + at] = m, p[4 + a.ws_rows + at] = l;
+      float* to = p + 4 + 2 * a.ws_rows + (int64_t)at * DP;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *(f32x4*)(to + t * 32 + c * 8 + h * 4) = f32x4{o[t][c * 4], o[t][c * 4 + 1], o[t][c * 4 + 2], o[t][c * 4 + 3]};
+    }
+  }
+
+  // ---- narrow tiles: up to 16 RT rows
+
+  // Every wave has all rows, and keys of its own: KT of every 4 KT.  They come into its own LDS, K and V each two turns ahead, waited for by count: no barrier, and as soon as a
+  // turn's K is read the next but one is on its way.  What the waves have is joined at the end.  (Where keys are read for few rows, memory is what bounds; the loads under way are what counts.)
+  __device__ __forceinline__ void run_narrow(int group, int part, int ends, int skip, int of, bool check, bool& again) {
+    constexpr int N = KT / 16, DN = DP / 16, SN32 = DP / 32;
+    constexpr int LK = N * SN::NI + (FP8 ? 1 : 0), LV = N * SN::NI;  // loads of a turn
+    const int G = a.group.d, col = lane & 15, kg = lane >> 4, rows = it.tokens * G;
+    const int k_begin = it.b0 * kAttnKeys, k_end = it.b1 * kAttnKeys;
+    Range keys = it.keys;                                          // (this item's share of them)
+    keys.lo = keys.lo > k_begin ? keys.lo : k_begin, keys.hi = keys.hi < k_end ? keys.hi : k_end;
+    const Range all = it.keys;
+    it.keys = keys;
+    s16x8 qn[RT][SN32];
+    int rlo[RT], rhi[RT];
+    float mx[RT], ls[RT];
+    f32x4 on[RT][DN];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      const int r = x * 16 + col, rr = r < rows ? r : rows - 1, i = (int)quotient(rr, a.group), g = rr - i * G;
+      const uint16_t* from = (const uint16_t*)a.q + (int64_t)(it.q.row0 + it.i0 + i) * a.qs.token + (int64_t)(it.head * G + g) * a.qs.head;
+#pragma unroll
+      for (int k = 0; k < SN32; ++k) {
+        const int c = k * 32 + kg * 8;
+        qn[x][k] = s16x8{};
+        if (r < rows && c < a.D) qn[x][k] = __builtin_bit_cast(s16x8, load_bits<u32x4>(from + c));
+      }
+      const Range mine = seen(a, it.q, it.i0 + i, it.i0 + i);
+      rlo[x] = mine.lo, rhi[x] = mine.hi;
+      mx[x] = -INFINITY, ls[x] = 0;
+#pragma unroll
+      for (int t = 0; t < DN; ++t) on[x][t] = f32x4{};
+    }
+    // keys that all rows see
+    const int all_lo = seen(a, it.q, it.i0 + it.tokens - 1, it.i0 + it.tokens - 1).lo, all_hi = seen(a, it.q, it.i0, it.i0).hi;
+    float lift = 1;
+    clear_lds();
+    uint32_t there[2];
+    auto issue_k = [&](int first, int turn) __attribute__((always_inline)) {
+      need_pages(first, KT);
+      uint32_t on = 0;
+#pragma unroll
+      for (int n = 0; n < N; ++n) on |= bring<FP8 ? 1 : 2>(false, first + n * 16, lds_at(&sh.own[wave][turn][0][n * 16 * NROW])) << n * 16;
+      there[turn] = on;
+      if constexpr (FP8) {                                         // lanes 0 .. 31: scales of K, the others: of V
+        int page, slot;
+        const bool is = where(first + (lane & 31), page, slot);
+        const float* from = (lane < 32 ? a.k_scales : a.v_scales) + ((int64_t)page * a.page.d + slot) * a.kv_heads + it.head;
+        load_lds4(is ? (const void*)from : (const void*)&kNothing, lds_at(&sh.scales[0][0][0]) + (wave * 2 + turn) * 256);
+      }
+    };
+    auto issue_v = [&](int first, int turn) __attribute__((always_inline)) {
+      need_pages(first, KT);                                       // (a key's pages are asked for again only if K has gone beyond them since)
+#pragma unroll
+      for (int n = 0; n < N; ++n) bring<FP8 ? 1 : 2>(true, first + n * 16, lds_at(&sh.own[wave][turn][1][n * 16 * NROW]));
+    };
+    auto body = [&](int first, int turn, int ahead) __attribute__((always_inline)) {
+      const uint8_t *K = sh.own[wave][turn][0], *V = sh.own[wave][turn][1];
+      const float* sc = &sh.scales[0][0][0] + (wave * 2 + turn) * 64;
+      const uint32_t is = there[turn];
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LV + LK) : "memory");
+      f32x4 s[RT][N];
+#pragma unroll
+      for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[x][n] = f32x4{};
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int k = 0; k < SN32; ++k) {
+          const int row = n * 16 + col;
+          s16x8 kf;
+          if constexpr (FP8) kf = widen<TYPE>(*(const u32x2*)(K + ((row * NROW + ((kg >> 1) ^ SN::place(false, row)) * 16 + (kg & 1) * 8) ^ (k * 32))));
+          else kf = *(const s16x8*)(K + ((row * NROW + (kg ^ SN::place(false, row)) * 16) ^ (k * 64)));
+#pragma unroll
+          for (int x = 0; x < RT; ++x) s[x][n] = mfma16<TYPE>(kf, qn[x][k], s[x][n]);
+        }
+      f32x4 vs[N];
+      if constexpr (FP8) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const f32x4 ks = *(const f32x4*)(sc + n * 16 + kg * 4);
+          vs[n] = *(const f32x4*)(sc + 32 + n * 16 + kg * 4);
+#pragma unroll
+          for (int x = 0; x < RT; ++x) s[x][n] *= ks;
+        }
+        if constexpr (TYPE == kF16) {                              // terms times scales stay in fp16's range: the scales relative to a power of two that the largest so far is below
+          const float mine = sc[32 + (lane & 31)], most = wave_all<Max>(fabsf(mine) <= 3.0e38f ? fabsf(mine) : 0.0f);
+          if (most > lift) {
+            const float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + 0x800000u), down = lift / to;
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+#pragma unroll
+              for (int t = 0; t < DN; ++t) on[x][t] *= down;
+            lift = to;
+          }
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // K is read: its place is free
+      issue_k(ahead, turn);
+      const bool masked = is != (N == 2 ? 0xffffffffu : 0xffffu) || first < all_lo || first + KT > all_hi;
+      s16x8 pk[RT];
+#pragma unroll
+      for (int x = 0; x < RT; ++x) {
+        if (masked) {
+#pragma unroll
+          for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int k = n * 16 + kg * 4 + e;
+              s[x][n][e] = first + k >= rlo[x] && first + k < rhi[x] && (is >> k & 1) ? s[x][n][e] : -INFINITY;
+            }
+        }
+        float top = fmaxf(fmaxf(s[x][0][0], s[x][0][1]), fmaxf(s[x][0][2], s[x][0][3]));
+        if constexpr (N == 2) top = fmaxf(top, fmaxf(fmaxf(s[x][N - 1][0], s[x][N - 1][1]), fmaxf(s[x][N - 1][2], s[x][N - 1][3])));
+        top = quarters<Max>(top) * a.scale_log2;
+        const float grown = fmaxf(mx[x], top);
+        if (__any(grown > mx[x])) {
+          const float by = grown > mx[x] ? exp2_fast(mx[x] - grown) : 1.0f;
+          mx[x] = grown, ls[x] *= by;
+#pragma unroll
+          for (int t = 0; t < DN; ++t) on[x][t] *= by;
+        }
+        const float less = LIFT - (mx[x] == -INFINITY ? 0.0f : mx[x]);
+        float p[4 * N];
+#pragma unroll
+        for (int e = 0; e < 4 * N; ++e) p[e] = exp2_fast(fmaf(s[x][e >> 2][e & 3], a.scale_log2, less));
+        if constexpr (!FP8) {
+#pragma unroll
+          for (int e = 0; e < 4 * N; ++e) ls[x] += p[e];
+        }
+        u32x4 w = {};
+        if constexpr (FP8) {
+          const float by = 1.0f / lift;
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const float v0 = vs[e >> 2][e & 3] * by, v1 = vs[e >> 2][e & 3 | 1] * by, t0 = p[e] * v0, t1 = p[e + 1] * v1;
+            w[e >> 1] = pack2<TYPE>(t0, t1);
+            ls[x] += weight(p[e], t0, v0, half<TYPE>(w[e >> 1], 0)) + weight(p[e + 1], t1, v1, half<TYPE>(w[e >> 1], 1));
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) w[e >> 1] = pack2<TYPE>(p[e], p[e + 1]);
+        }
+        pk[x] = __builtin_bit_cast(s16x8, w);
+      }
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LK + LV) : "memory");
+#pragma unroll
+      for (int t = 0; t < DN; ++t) {
+        if constexpr (FP8) {
+          const int j = col >> 1, row = 16 * (j >> 2) + 4 * kg + (j & 3);
+          const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((tr8_ptr)(V + ((row * NROW + SN::place(true, row) * 16 + (col & 1) * 8) ^ (t * 16))));
+          const s16x8 vf = widen<TYPE>(u32x2{(uint32_t)v[0], (uint32_t)v[1]});
+#pragma unroll
+          for (int x = 0; x < RT; ++x) on[x][t] = mfma16<TYPE>(vf, pk[x], on[x][t]);
+        } else {
+          const int row = 4 * kg + (col >> 2);
+          const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(V + ((row * NROW + (((col & 3) >> 1) ^ SN::place(true, row)) * 16 + (col & 1) * 8) ^ (t * 32))));
+#pragma unroll
+          for (int x = 0; x < RT; ++x) on[x][t] = mfma16_short<TYPE>(v, s16x4{pk[x][0], pk[x][1], pk[x][2], pk[x][3]}, on[x][t]);
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      issue_v(ahead, turn);
+    };
+    const int step = 4 * KT, first = k_begin + wave * KT;
+    issue_k(first, 0), issue_v(first, 0), issue_k(first + step, 1), issue_v(first + step, 1);
+    for (int at = k_begin; at < k_end; at += 2 * step) {
+      body(at + wave * KT, 0, at + wave * KT + 2 * step);
+      if (at + step < k_end) body(at + step + wave * KT, 1, at + wave * KT + 3 * step);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    it.keys = all;
+    float bad = 0;
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      ls[x] = quarters<Add>(ls[x]);
+#pragma unroll
+      for (int t = 0; t < DN; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad = fmaf(on[x][t][e], 0.0f, bad);
+    }
+    again = check && not_finite(bad);
+    lds_barrier();                                                 // (the turns are free)
+    if (again) return;
+    // the waves' results, 16 bytes changing places by the row
+    float* mine = (float*)&sh.kv[0][0][0] + wave * (RT * 16 * DP);
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      const int r = x * 16 + col;
+      if (kg == 0) sh.top[wave][r] = mx[x], sh.sum[wave][r] = ls[x];
+#pragma unroll
+      for (int t = 0; t < DN; ++t) *(f32x4*)(mine + r * DP + ((t * 4 + kg) ^ (r & 7)) * 4) = on[x][t] * lift;
+    }
+    lds_barrier();
+    constexpr int PER = DP / 64;                                   // f32x4 of a thread: 16 threads a row
+    float* p = part < 0 ? nullptr : a.ws + part_at(a, group, part, DP);
+    if (p && threadIdx.x == 0) *(u32x4*)p = u32x4{(uint32_t)(1 | ends << 1), (uint32_t)(it.q.row0 + it.i0 - skip), (uint32_t)it.head, (uint32_t)(of * G)};
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      const int r = x * 16 + (int)(threadIdx.x >> 4), c = threadIdx.x & 15;
+      if (r >= rows) break;
+      const float top = fmaxf(fmaxf(sh.top[0][r], sh.top[1][r]), fmaxf(sh.top[2][r], sh.top[3][r])), base = top == -INFINITY ? 0.0f : top;
+      float sum = 0;
+      f32x4 v[PER];
+#pragma unroll
+      for (int k = 0; k < PER; ++k) v[k] = f32x4{};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float by = exp2_fast(sh.top[w][r] - base);
+        sum += sh.sum[w][r] * by;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) v[k] += *(const f32x4*)((float*)&sh.kv[0][0][0] + (w * RT * 16 + r) * DP + ((c * PER + k) ^ (r & 7)) * 4) * by;
+      }
+      if (p) {
+        const int at = skip * G + r;
+        if (c == 0) p[4 + at] = top, p[4 + a.ws_rows + at] = sum;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) *(f32x4*)(p + 4 + 2 * a.ws_rows + (int64_t)at * DP + (c * PER + k) * 4) = v[k];
+      } else {
+        const float by = sum == 0 ? 0.0f : 1.0f / sum;
+        const int i = (int)quotient(r, a.group), g = r - i * G;
+        uint16_t* to = (uint16_t*)a.out + (int64_t)(it.q.row0 + it.i0 + i) * a.os.token + (int64_t)(it.head * G + g) * a.os.head;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+          const int at = (c * PER + k) * 4;
+          if (at < a.D) store_bits(to + at, u32x2{pack2<TYPE>(v[k][0] * by, v[k][1] * by), pack2<TYPE>(v[k][2] * by, v[k][3] * by)});
+        }
+      }
+    }
+    lds_barrier();
+  }
+
+  // Values of keys that some rows of a tile see and others do not: the product has them in all rows, times 0, which is not 0 if they are not finite.  So where something that is not finite has come
+  // out, the tokens are done one by one: a token's rows see the same keys, and the others are zeros in LDS.
+  __device__ __forceinline__ void work(int group, int part, int ends) {
+    const int i0 = it.i0, tokens = it.tokens;
+    for (int i = -1; i < tokens; ++i) {
+      if (i >= 0) it.i0 = i0 + i, it.tokens = 1, it.keys = seen(a, it.q, it.i0, it.i0);
+      const bool check = i < 0 && a.causal && tokens > 1;
+      const int skip = i < 0 ? 0 : i;
+      bool again = false;
+      page0 = -1000;
+      if constexpr (RT > 0) run_narrow(group, part, ends, skip, tokens, check, again);
+      else {
+        run_wide();
+        again = check && not_finite(check_wide());
+        lds_barrier();                                             // (the stages are free)
+        if (!again) finish_wide(group, part, ends, skip, tokens);
+      }
+      if (i < 0 && !again) break;
+    }
+  }
+
+  __device__ __forceinline__ void tile(int tile, int tokens) {
+    it.i0 = tile * tokens;
+    it.tokens = it.i0 + tokens < it.q.n ? tokens : it.q.n - it.i0;
+    it.keys = seen(a, it.q, it.i0, it.i0 + it.tokens - 1);
+  }
+
+  // Sum of v over the workgroup's threads before this one, and of all.
+  __device__ __forceinline__ int64_t scan(int64_t v, int64_t& total) {
+    int64_t x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t y = __shfl_up(x, d);
+      if (lane >= d) x += y;
+    }
+    lds_barrier();
+    if (lane == 63) sh.sums[wave] = x;
+    lds_barrier();
+    int64_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) before += sh.sums[w];
+      total += sh.sums[w];
+    }
+    return before + x - v;
+  }
+
+  // Every workgroup a tile, the last of a sequence first (they see the most keys); a head's tiles go to workgroups that share an XCD where 8 divides the heads.
+  __device__ __forceinline__ void whole_tiles() {
+    const int tokens = ROWS / a.group.d;
+    const int64_t number = a.t0 + blockIdx.x, want = number / a.kv_heads;
+    it.head = (int)(number - want * a.kv_heads);
+    int64_t carry = 0;
+    if (threadIdx.x == 0) sh.found[0] = -1;
+    for (int base = 0; base < a.S; base += 256) {                  // sequences from the last on
+      const int s = a.S - 1 - base - (int)threadIdx.x;
+      const int n = s >= 0 ? tiles_of(a, sequence(a, s), tokens) : 0;
+      int64_t total;
+      const int64_t before = carry + scan(n, total);
+      if (want >= before && want < before + n) sh.found[0] = s, sh.found[1] = n - 1 - (want - before);
+      carry += total;
+      lds_barrier();
+      if (want < carry) break;
+    }
+    const int s = __builtin_amdgcn_readfirstlane((int)sh.found[0]), t = __builtin_amdgcn_readfirstlane((int)sh.found[1]);
+    if (s < 0) return;
+    it.s = s;
+    it.q = sequence(a, s);
+    tile(t, tokens);
+    const Blocks b = blocks_of(it.keys);
+    it.b0 = b.first, it.b1 = b.first + b.count;
+    work(0, -1, 0);
+  }
+
+  // A run of the list of all blocks.
+  __device__ __forceinline__ void split() {
+    const int tokens = ROWS / a.group.d, groups = a.groups;
+    // neighbours in the list share keys: they go to one XCD
+    const int group = (int)(blockIdx.x & 7) * (groups >> 3) + (int)(blockIdx.x >> 3);
+    int64_t* before = (int64_t*)&sh.kv[0][0][0];                   // of the sequences, in blocks of one head
+    int64_t carry = 0;
+    for (int base = 0; base < a.S; base += 256) {
+      const int s = base + (int)threadIdx.x;
+      Cost c = {0, 0};
+      if (s < a.S) c = cost_of(a, sequence(a, s), tokens);
+      int64_t total;
+      const int64_t at = scan((int64_t)c.pairs * c.cell, total);
+      if (s < a.S) before[s] = carry + at;
+      carry += total;
+    }
+    lds_barrier();
+    const int64_t all = carry * a.kv_heads;
+    const int64_t busy = all < groups ? all : groups;              // (each of them has a block at least: parts of a tile lie in neighbouring workgroups' places)
+    int wrote = 0;                                                 // parts
+    auto done = [&]() __attribute__((always_inline)) {
+      if (threadIdx.x < 2 && !(wrote >> threadIdx.x & 1)) *(uint32_t*)(a.ws + part_at(a, group, threadIdx.x, DP)) = 0;
+    };
+    if (group >= busy) return done();
+    int64_t u = all * group / busy;
+    const int64_t end = all * (group + 1) / busy;
+    for (int s = threadIdx.x; s < a.S; s += 256) {
+      const int64_t to = s + 1 < a.S ? before[s + 1] : carry;
+      if (before[s] * a.kv_heads <= u && u < to * a.kv_heads) sh.found[0] = s, sh.found[1] = before[s];
+    }
+    lds_barrier();
+    int s = __builtin_amdgcn_readfirstlane((int)sh.found[0]);
+    int64_t rest = u - sh.found[1] * a.kv_heads;
+    lds_barrier();
+    it.s = s, it.q = sequence(a, s);
+    Cost c = cost_of(a, it.q, tokens);
+    int64_t of_head = (int64_t)c.pairs * c.cell;
+    it.head = __builtin_amdgcn_readfirstlane((int)(rest / of_head));
+    rest -= it.head * of_head;
+    int pair = __builtin_amdgcn_readfirstlane((int)(rest / c.cell)), at = __builtin_amdgcn_readfirstlane((int)(rest - (int64_t)pair * c.cell));
+    while (u < end) {
+      const int tiles = tiles_of(a, it.q, tokens), lastt = tiles - 1 - pair;
+      const int n0 = tile_blocks(a, it.q, tokens, pair).count, n1 = lastt > pair ? tile_blocks(a, it.q, tokens, lastt).count : 0;
+      if (at < n0 + n1) {
+        const bool second = at >= n0;
+        tile(second ? lastt : pair, tokens);
+        const Blocks b = blocks_of(it.keys);
+        const int from = second ? at - n0 : at;
+        const int64_t left = end - u;
+        const int to = b.count - from <= left ? b.count : from + (int)left;
+        it.b0 = b.first + from, it.b1 = b.first + to;
+        const bool starts = from == 0, ends = to == b.count;
+        work(group, starts && ends ? -1 : starts ? 1 : 0, ends);
+        if (!(starts && ends)) wrote |= starts ? 2 : 1;
+        u += to - from, at += to - from;
+      }
+      if (at >= n0 + n1) {                                         // the next pair, head, sequence
+        u += c.cell - at, at = 0;
+        if (u >= end) break;
+        if (++pair == c.pairs) {
+          pair = 0;
+          if (++it.head == a.kv_heads) {
+            it.head = 0;
+            do {
+              if (++it.s >= a.S) return done();
+              it.q = sequence(a, it.s);
+              c = cost_of(a, it.q, tokens);
+            } while (c.pairs == 0);
+          }
+        }
+      }
+    }
+    done();
+  }
+};
+
+template <int TYPE, bool FP8, int DP, int RT, bool SPLIT>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void cache_attention_kernel(CacheArgs a) {
+  using A = Attention<TYPE, FP8, DP, RT>;
+  __shared__ typename A::Shared sh;
+  A w(a, sh);
+  if constexpr (SPLIT) w.split();
+  else w.whole_tiles();
+}
+
+// By types and columns.
+template <int RT, bool SPLIT, int TYPE, bool FP8>
+void launch_attention_columns(const CacheArgs& a, uint32_t groups, hipStream_t s) {
+  const int dp = attn_columns(a.D);
+  if (dp == 64) cache_attention_kernel<TYPE, FP8, 64, RT, SPLIT><<<groups, 256, 0, s>>>(a);
+  else if (dp == 128) cache_attention_kernel<TYPE, FP8, 128, RT, SPLIT><<<groups, 256, 0, s>>>(a);
+  else cache_attention_kernel<TYPE, FP8, 256, RT, SPLIT><<<groups, 256, 0, s>>>(a);
+}
+template <int RT, bool SPLIT>
+void launch_attention(const CacheArgs& a, uint32_t groups, hipStream_t s) {
+  if (a.type == kBf16) a.fp8 ? launch_attention_columns<RT, SPLIT, kBf16, true>(a, groups, s) : launch_attention_columns<RT, SPLIT, kBf16, false>(a, groups, s);
+  else a.fp8 ? launch_attention_columns<RT, SPLIT, kF16, true>(a, groups, s) : launch_attention_columns<RT, SPLIT, kF16, false>(a, groups, s);
+}
+
+}  // namespace axe

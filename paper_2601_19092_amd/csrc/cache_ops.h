@@ -41,37 +41,51 @@ struct CacheArgs {
   int32_t causal, window;
   float scale_log2;                // scale / ln 2
   int32_t type, fp8;               // kBf16 or kF16; e4m3 cache
+  int32_t sixteens;                // attention: 16 keys from a multiple of 16 on lie in one page, within 2^31 bytes of each other
   int32_t groups;                  // attention, split form: workgroups
+  int32_t tile_rows;               // 16, 32 or kAttnRows
   int32_t ws_rows;                 // rows of a partial result
 };
 hipError_t launch_cache_append(const CacheArgs& a, hipStream_t s);
 hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t s);
 
+template <int RT>
+void launch_attention_narrow(const CacheArgs& a, hipStream_t s);
+template <>
+void launch_attention_narrow<1>(const CacheArgs& a, hipStream_t s);
+template <>
+void launch_attention_narrow<2>(const CacheArgs& a, hipStream_t s);
+
 // ---- attention: the shape of a call
 
-constexpr int kAttnRows = 128;     // rows (tokens x query heads of one head of the cache) of a tile
+constexpr int kAttnRows = 128;     // rows (tokens x query heads of one head of the cache) of a wide tile
 constexpr int kAttnKeys = 64;      // keys of a block
 constexpr int kAttnMaxGroup = 128; // query heads of a head of the cache
 constexpr int kAttnSplitSeqs = 4096;
 
 inline int attn_columns(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
-inline int attn_tile_tokens(int group) { return kAttnRows / group; }
 // Workgroups that the chip holds at once.
 inline int attn_slots(int D) { return attn_columns(D) <= 128 ? 512 : 256; }
-// Whether the keys of a tile are split among workgroups: not where there are tiles enough to fill the chip some times over, each a workgroup's.
-inline bool attn_split(int64_t T, int S, int kv_heads, int group, int D) {
-  const int64_t tokens = attn_tile_tokens(group), tiles = (T + tokens - 1) / tokens * kv_heads;
-  return S <= kAttnSplitSeqs && tiles < 2 * (int64_t)attn_slots(D);
-}
-inline int attn_ws_rows(int64_t T, int group) {
-  const int64_t rows = T < attn_tile_tokens(group) ? T * group : kAttnRows;
-  return (int)((rows + 31) / 32 * 32);
+
+// groups: workgroups of the split form, 0: every tile a workgroup's.  The keys of a tile are split among workgroups unless there are tiles enough to fill the chip some times over.
+// Rows of a tile: as many as the sequences have on average, up to 32; from there on 128.
+struct AttnShape {
+  int tile_rows, groups, ws_rows;
+};
+inline AttnShape attn_shape(int64_t T, int S, int kv_heads, int group, int D) {
+  AttnShape r = {kAttnRows, 0, 0};
+  if (T == 0 || S == 0) return r;
+  const int64_t wide = kAttnRows / group, tiles = (T + wide - 1) / wide * kv_heads;
+  if (S > kAttnSplitSeqs || tiles >= 2 * (int64_t)attn_slots(D)) return r;
+  const int64_t rows = (T + S - 1) / S * group;
+  if (rows <= 32) r.tile_rows = rows <= 16 ? 16 : 32;
+  r.groups = attn_slots(D);
+  const int64_t tokens = r.tile_rows / group, most = T < tokens ? T * group : r.tile_rows;
+  r.ws_rows = (int)((most + 15) / 16 * 16);
+  return r;
 }
 // A partial result: a head of four words, the maxima and sums of its rows, the rows themselves.
 inline int64_t attn_part_words(int rows, int D) { return 4 + 2 * (int64_t)rows + (int64_t)rows * attn_columns(D); }
-inline int64_t attn_workspace_words(int64_t T, int S, int kv_heads, int group, int D) {
-  if (T == 0 || !attn_split(T, S, kv_heads, group, D)) return 0;
-  return 2 * attn_slots(D) * attn_part_words(attn_ws_rows(T, group), D);
-}
+inline int64_t attn_workspace_words(const AttnShape& s, int D) { return 2 * s.groups * attn_part_words(s.ws_rows, D); }
 
 }  // namespace axe

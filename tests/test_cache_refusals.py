@@ -58,7 +58,7 @@ def test_sizes_and_types(rc):
     assert rc(set_={"q_heads": 5}) == B.AXE_EINVAL
     assert rc(dt=9) == B.AXE_EINVAL and rc(cache=9) == B.AXE_EINVAL and rc(dt=B.AXE_FP8_E4M3) == B.AXE_EINVAL
     assert rc(dt=B.AXE_F32) == B.AXE_EUNSUPPORTED and rc(dt=B.AXE_BF16, cache=B.AXE_F16) == B.AXE_EUNSUPPORTED and rc(dt=B.AXE_F16, cache=B.AXE_F32) == B.AXE_EUNSUPPORTED
-    assert rc(D=60) == B.AXE_EUNSUPPORTED and rc(D=264) == B.AXE_EUNSUPPORTED
+    assert rc(D=60) == B.AXE_EUNSUPPORTED and rc(D=264) == B.AXE_EUNSUPPORTED and rc(D=72, cache=B.AXE_FP8_E4M3) == B.AXE_EUNSUPPORTED
     assert rc(Hq=129, Hkv=1) == B.AXE_EUNSUPPORTED
     assert rc(set_={"max_pages": 1 << 28, "page_tokens": 1 << 10}) == B.AXE_EUNSUPPORTED and rc(set_={"S": 1 << 20}) == B.AXE_EUNSUPPORTED
     assert rc(set_={"T": (1 << 30) + 1}) == B.AXE_EUNSUPPORTED and rc(set_={"pages": (1 << 30) + 1}) == B.AXE_EUNSUPPORTED

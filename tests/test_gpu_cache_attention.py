@@ -50,7 +50,7 @@ class Batch:
             strides[ax] = step
             step *= dims[ax]
         self.strides = (strides["p"], strides["s"], strides["h"], 1)
-        self.layout = B.Layout(W.spec([(self.pages, strides["p"], "m"), (page, strides["s"], "m"), (Hkv, strides["h"], "m"), (D, 1, "m")], O={"m": 8}), ["m"])
+        self.layout = B.Layout(W.spec([(self.pages, strides["p"], "m"), (page, strides["s"], "m"), (Hkv, strides["h"], "m"), (D, 1, "m")], O={"m": 16}), ["m"])
         self.kv, self.scales, self.values = [], [], []
         for _ in range(2):
             x = torch.randn((self.pages, page, Hkv, D), generator=g)
@@ -67,8 +67,8 @@ class Batch:
                 x = (x / sc[..., None]).clamp(-448, 448)
             x = x.to(TORCH[self.cache])
             self.values.append(f64(x) * (1.0 if sc is None else f64(sc)[..., None]))
-            buf = torch.zeros(8 + step + 64, dtype=TORCH[self.cache])
-            (torch.as_strided(buf.view(torch.uint8), x.shape, self.strides, 8).copy_(x.view(torch.uint8)) if self.cache == "fp8" else torch.as_strided(buf, x.shape, self.strides, 8).copy_(x))
+            buf = torch.zeros(16 + step + 64, dtype=TORCH[self.cache])
+            (torch.as_strided(buf.view(torch.uint8), x.shape, self.strides, 16).copy_(x.view(torch.uint8)) if self.cache == "fp8" else torch.as_strided(buf, x.shape, self.strides, 16).copy_(x))
             self.kv.append(buf.cuda())
             self.scales.append(None if sc is None else sc.contiguous().cuda())
 
@@ -102,9 +102,14 @@ class Batch:
 
 
 @pytest.mark.parametrize("dtype, cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "fp8"), ("f16", "fp8")])
-@pytest.mark.parametrize("D", [64, 128, 256, 8, 80])
-def test_types_and_columns(dtype, cache, D):
-    b = Batch([130, 1, 77], [3, 1, 70], 4, 2, D, 16, dtype, cache, seed=D)
+@pytest.mark.parametrize("D", [64, 128, 256, 16, 80, 8, 136])
+@pytest.mark.parametrize("new", [[3, 1, 70], [1, 1, 1], [9, 8, 7]])    # tiles of 128, 16 and 32 rows
+def test_types_and_columns(dtype, cache, D, new):
+    if cache == "fp8" and D % 16:
+        with pytest.raises(B.AxeError, match="head_dim"):
+            Batch([130, 8, 77], new, 4, 2, D, 16, dtype, cache, seed=D).run()
+        return
+    b = Batch([530, 8, 77], new, 4, 2, D, 16, dtype, cache, seed=D)
     b.check(b.run())
 
 
