@@ -75,6 +75,14 @@ __device__ __forceinline__ float half(uint32_t two, int which) {
   if constexpr (TYPE == kBf16) return __uint_as_float(which ? two & 0xffff0000u : two << 16);
   else return (float)__builtin_bit_cast(_Float16, (uint16_t)(two >> which * 16));
 }
+// Their sum, and c.
+template <int TYPE>
+__device__ __forceinline__ float add2(uint32_t two, float c) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+  if constexpr (TYPE == kBf16) return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3f803f80u), c, false);
+  else return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, two), f16x2{(_Float16)1.0f, (_Float16)1.0f}, c, false);
+}
 // What a term p counts in the sum when the product with V has t = p v, v the scale of V's row, as `rounded`: rounded / v.  A key that has nearly all the weight then has V's row for its result, not that times
 // the error of one rounding.
 __device__ __forceinline__ float weight(float p, float t, float v, float rounded) {
@@ -100,13 +108,28 @@ __device__ const u32x4 kNothing = {0, 0, 0, 0};
 
 // Loads into LDS, 16 bytes a lane: the wave's 1024 bytes from `lds` on.  (Written as asm: the compiler would wait for them before it reads any of LDS.  M0 holds the address;
 // the wait states are for registers that a vector instruction may just have written.)
+template <bool ONCE>
 __device__ __forceinline__ void load_lds(const void* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory");
+  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "s"(lds) : "memory");
+  else asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory");
 }
+template <bool ONCE>
 __device__ __forceinline__ void load_lds(uint32_t offset, const void* base, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
+  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(offset), "s"(base), "s"(lds) : "memory");
+  else asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
 }
-
+// Two of them, the second's 1024 bytes behind the first's.
+template <bool ONCE>
+__device__ __forceinline__ void load_lds(uint32_t offset, uint32_t offset2, const void* base, uint32_t lds) {
+  if constexpr (ONCE)
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %2 nt\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"v"(offset), "v"(offset2),
+                 "s"(base), "s"(lds)
+                 : "memory", "scc");
+  else
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %2\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"v"(offset), "v"(offset2), "s"(base),
+                 "s"(lds)
+                 : "memory", "scc");
+}
 // The same, 4 bytes a lane.
 __device__ __forceinline__ void load_lds4(const void* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(lds) : "memory");
@@ -199,14 +222,25 @@ struct Attention {
   static constexpr int BLOCK = kAttnKeys * ROW;                    // of K, or V, of a block
   static constexpr int STEPS = DP / 16, DT = DP / 32;
   // exp2 of this is a factor of the softmax's terms: fp16 has few numbers below 1
-  static constexpr float LIFT = TYPE == kBf16 ? 0.0f : FP8 ? 8.0f : 15.0f;
+  static constexpr float LIFT = TYPE == kBf16 ? 0.0f : 9.0f;
+  // The running maximum is left alone until a score is this much (in powers of two) above it: terms are up to 2^LAG, and hardly ever is all that has been summed multiplied down.
+  static constexpr float LAG = 6.0f;
 
   // Sixteen keys as loads of 16 bytes a lane bring them to LDS: CH chunks a key, RPI keys a load, NI loads.  Chunks change places by the key's number, so that what is read
   // together lies in different banks.
   template <int EB>
   struct Sixteen {
     static constexpr int CH = DP * EB / 16, RPI = 64 / CH, NI = 16 / RPI;
-    static __device__ __forceinline__ int place(bool v, int row) { return EB == 1 ? (CH >= 8 ? row & 7 : row >> 1 & 3) : v ? (row & 3) << 1 : row & 7; }
+    static constexpr int LINE = CH >= 16 ? 1 : 16 / CH;            // keys that lie in 256 bytes, the width of LDS
+    // What a key's chunks are moved by (XOR).  K is read by 16 lanes at a time, the same chunk of 16 keys.
+    static __device__ __forceinline__ int k(int row) { return row / LINE & (CH < 16 ? CH - 1 : 15); }
+    // V, wide: by 32 lanes, 64 bytes of 4 keys; narrow: 32 bytes of 8 keys; narrow in e4m3: 16 bytes of 16 keys, those of 16 .. with those of 0 ..
+    static __device__ __forceinline__ int v(int row) {
+      if constexpr (EB == 1) return (row % 8 / LINE | (row >> 4 & 1) * (8 / LINE)) & (CH < 16 ? CH - 1 : 15);
+      else if constexpr (RT == 0) return (row % 4 / LINE << 2) & (CH - 1);
+      else return (row % 8 / LINE << 1) & (CH - 1);
+    }
+    static __device__ __forceinline__ int place(bool of_v, int row) { return of_v ? v(row) : k(row); }
   };
   using S2 = Sixteen<2>;
   using SN = Sixteen<FP8 ? 1 : 2>;
@@ -267,38 +301,54 @@ struct Attention {
     slot = in ? key - p * (int)a.page.d : 0;
     return in && (uint32_t)page < (uint64_t)a.pages;
   }
-  // Sixteen keys (K or V) to LDS.  Returns which there are.
+  // Where sixteen keys lie.
+  struct Found {
+    int first, page, slot;
+    bool side_by_side;
+  };
+  __device__ __forceinline__ Found find(int first) {
+    Found f = {first, 0, 0, false};
+    f.side_by_side = together(first, f.page, f.slot);
+    return f;
+  }
+  // Sixteen keys (K or V) to LDS, as keys row0 .. there.
   template <int EB>
-  __device__ __forceinline__ uint32_t bring(bool v, int first, uint32_t lds) {
+  __device__ __forceinline__ void bring(bool v, const Found& f, int row0, uint32_t lds) {
     using S = Sixteen<EB>;
+    constexpr bool ONCE = RT > 0;
     const CachePlaces& pl = v ? a.vp : a.kp;
     const uint8_t* cache = (const uint8_t*)(v ? a.v_cache : a.k_cache) + (int64_t)it.head * pl.head * EB;
-    int page, slot;
-    if (together(first, page, slot)) {
-      const uint8_t* base = cache + (page * pl.page + slot * pl.slot) * EB;
+    auto column = [&](int i) __attribute__((always_inline)) { return (lane % S::CH ^ S::place(v, row0 + i * S::RPI + lane / S::CH)) * 16; };
+    if (f.side_by_side) {
+      const uint8_t* base = cache + (f.page * pl.page + f.slot * pl.slot) * EB;
+      auto offset = [&](int i) __attribute__((always_inline)) { return (uint32_t)((i * S::RPI + lane / S::CH) * (int)pl.slot * EB + column(i)); };
+      if (a.D == DP) {
+        if constexpr (S::NI == 1) load_lds<ONCE>(offset(0), base, lds);
+        else
 #pragma unroll
-      for (int i = 0; i < S::NI; ++i) {
-        const int row = i * S::RPI + lane / S::CH, c = (lane % S::CH ^ S::place(v, row)) * 16;
-        const uint32_t off = (uint32_t)(row * (int)pl.slot * EB + c);
-        if (DP == 128 || c < a.D * EB) load_lds(off, base, lds + i * 1024);   // (the others' places hold zeros, see clear_lds)
+          for (int i = 0; i < S::NI; i += 2) load_lds<ONCE>(offset(i), offset(i + 1), base, lds + i * 1024);
+      } else {
+#pragma unroll
+        for (int i = 0; i < S::NI; ++i)                            // (the other lanes' places hold zeros, see clear_lds)
+          if (column(i) < a.D * EB) load_lds<ONCE>(offset(i), base, lds + i * 1024);
       }
-      return 0xffff;
+      return;
     }
-    uint32_t there = 0;
+    const bool any = f.first < it.keys.hi && f.first + 16 > it.keys.lo;
+    int page, slot;
 #pragma unroll
     for (int i = 0; i < S::NI; ++i) {
-      const int row = i * S::RPI + lane / S::CH, c = (lane % S::CH ^ S::place(v, row)) * 16;
-      const bool on = where(first + row, page, slot);
-      const uint8_t* from = cache + (page * pl.page + slot * pl.slot) * EB + c;
-      load_lds(on && c < a.D * EB ? (const void*)from : (const void*)&kNothing, lds + i * 1024);
-      there |= on ? 1u << row : 0u;
+      const void* from = &kNothing;
+      if (any && where(f.first + i * S::RPI + lane / S::CH, page, slot) && column(i) < a.D * EB) from = cache + (page * pl.page + slot * pl.slot) * EB + column(i);
+      load_lds<false>(from, lds + i * 1024);
     }
-    return wave_or(there);
   }
-  static __device__ __forceinline__ uint32_t wave_or(uint32_t v) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v |= (uint32_t)__shfl_xor((int)v, d);
-    return (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+  // Which of KEYS keys there are.
+  template <int KEYS>
+  __device__ __forceinline__ uint32_t which(int first) {
+    if (first >= it.keys.hi || first + KEYS <= it.keys.lo) return 0;
+    int page, slot;
+    return (uint32_t)__ballot(where(first + lane, page, slot) && lane < KEYS);
   }
   // Columns from D to DP stay zero: nothing is loaded there.
   __device__ __forceinline__ void clear_lds() {
@@ -313,7 +363,7 @@ struct Attention {
   f32x16 o[RT ? 1 : DT];
   float m, l;                                                      // running maximum (scaled) and this lane's part of the sum
   int lo, hi;                                                      // keys that this lane's row sees
-  int w_lo, w_hi_all, w_lo_all, w_hi;                              // of the wave's rows: seen by any, by all
+  int w_lo, w_hi;                                                  // that all of the wave's rows see
   bool rows_here;
   float lift_v;                                                    // e4m3 values in fp16: what their scales are divided by, a power of two
   u32x2 kreg[FP8 ? S2::NI : 1], vreg[FP8 ? S2::NI : 1];            // e4m3: a block on its way
@@ -323,17 +373,17 @@ struct Attention {
   __device__ __forceinline__ void issue(int block, int stage) {
     const int first = block * kAttnKeys + wave * 16;
     need_pages(first, 16);
-    uint32_t there = 0;
+    const Found f = find(first);
+    const uint32_t there = f.side_by_side ? 0xffff : which<16>(first);
     if constexpr (!FP8) {
-      there = bring<2>(false, first, lds_at(&sh.kv[stage][0][wave * 16 * ROW]));
-      bring<2>(true, first, lds_at(&sh.kv[stage][1][wave * 16 * ROW]));
+      bring<2>(false, f, 0, lds_at(&sh.kv[stage][0][wave * 16 * ROW]));
+      bring<2>(true, f, 0, lds_at(&sh.kv[stage][1][wave * 16 * ROW]));
     } else {
       int page, slot;
 #pragma unroll
       for (int i = 0; i < S2::NI; ++i) {
         const int row = i * S2::RPI + lane / S2::CH, kc = (lane % S2::CH ^ S2::place(false, row)) * 8, vc = (lane % S2::CH ^ S2::place(true, row)) * 8;
         const bool on = where(first + row, page, slot);
-        there |= on ? 1u << row : 0u;
         const int64_t kat = page * a.kp.page + slot * a.kp.slot + it.head * a.kp.head, vat = page * a.vp.page + slot * a.vp.slot + it.head * a.vp.head;
         kreg[i] = vreg[i] = u32x2{};
         if (on && kc < a.D) kreg[i] = *(const u32x2*)((const uint8_t*)a.k_cache + kat + kc);
@@ -345,7 +395,6 @@ struct Attention {
         const int64_t at = ((int64_t)page * a.page.d + slot) * a.kv_heads + it.head;
         sreg[0] = a.k_scales[at], sreg[1] = a.v_scales[at];
       }
-      there = wave_or(there);
     }
     if (lane == 0) sh.there[stage][wave] = (uint16_t)there;
   }
@@ -378,9 +427,8 @@ struct Attention {
     const Range mine = seen(a, it.q, it.i0 + i, it.i0 + i);
     lo = mine.lo, hi = mine.hi;
     const int last = rows - 1 < wave * 32 + 31 ? rows - 1 : wave * 32 + 31;
-    const Range f = seen(a, it.q, it.i0 + (int)quotient(rows_here ? wave * 32 : 0, a.group), it.i0 + (int)quotient(rows_here ? wave * 32 : 0, a.group));
-    const Range b = seen(a, it.q, it.i0 + (int)quotient(last, a.group), it.i0 + (int)quotient(last, a.group));
-    w_lo = f.lo, w_lo_all = b.lo, w_hi_all = f.hi, w_hi = b.hi;    // (both ends grow with the token)
+    w_lo = seen(a, it.q, it.i0 + (int)quotient(last, a.group), it.i0 + (int)quotient(last, a.group)).lo;   // (both ends grow with the token)
+    w_hi = seen(a, it.q, it.i0 + (int)quotient(rows_here ? wave * 32 : 0, a.group), it.i0 + (int)quotient(rows_here ? wave * 32 : 0, a.group)).hi;
     m = -INFINITY, l = 0, lift_v = 1;
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = f32x16{};
@@ -389,14 +437,13 @@ struct Attention {
   // A block's share of the wave's rows, from a stage.
   __device__ __forceinline__ void compute(int block, int stage) {
     const int k0 = block * kAttnKeys;
-    if (!rows_here || k0 >= w_hi || k0 + kAttnKeys <= w_lo) return;
     const uint64_t there = *(const uint64_t*)&sh.there[stage][0];
     const uint32_t t0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)there), t1 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(there >> 32));
-    const bool masked = (t0 & t1) != 0xffffffffu || k0 < w_lo_all || k0 + kAttnKeys > w_hi_all;
+    const bool masked = (t0 & t1) != 0xffffffffu || k0 < w_lo || k0 + kAttnKeys > w_hi;
     const uint8_t *K = sh.kv[stage][0], *V = sh.kv[stage][1];
     f32x16 s[2] = {f32x16{}, f32x16{}};
     {
-      const uint32_t at = (lane & 31) * ROW + (h ^ S2::place(false, lane & 31)) * 16;
+      const uint32_t at = (lane & 31) * ROW + (h ^ S2::k(lane & 31)) * 16;
 #pragma unroll
       for (int k = 0; k < STEPS; ++k) {
 #pragma unroll
@@ -429,9 +476,8 @@ struct Attention {
 #pragma unroll
     for (int r = 1; r < 32; ++r) top = fmaxf(top, s[r >> 4][r & 15]);
     top = fmaxf(top, other_half(top)) * a.scale_log2;
-    const float grown = fmaxf(m, top);
-    if (__any(grown > m)) {
-      const float by = grown > m ? exp2_fast(m - grown) : 1.0f;    // (the first time: m is -inf, the sums are 0)
+    if (__any(top > m + LAG)) {
+      const float grown = fmaxf(m, top), by = grown > m ? exp2_fast(m - grown) : 1.0f;   // (the first time: m is -inf, the sums are 0)
       m = grown, l *= by;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
@@ -442,10 +488,7 @@ struct Attention {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[t][r] = exp2_fast(fmaf(s[t][r], a.scale_log2, less));
-        if constexpr (!FP8) l += s[t][r];
-      }
+      for (int r = 0; r < 16; ++r) s[t][r] = exp2_fast(fmaf(s[t][r], a.scale_log2, less));
     float by_v = 1;
     if constexpr (FP8 && TYPE == kF16) {                           // as in run_narrow
       const float sv = sh.scales[stage][1][lane], most = wave_all<Max>(fabsf(sv) <= 3.0e38f ? fabsf(sv) : 0.0f);
@@ -472,13 +515,16 @@ struct Attention {
           const float v0 = sc[0] * by_v, v1 = sc[1] * by_v, t0 = x * v0, t1 = y * v1;
           w[e] = pack2<TYPE>(t0, t1);
           l += weight(x, t0, v0, half<TYPE>(w[e], 0)) + weight(y, t1, v1, half<TYPE>(w[e], 1));
-        } else w[e] = pack2<TYPE>(x, y);
+        } else {
+          w[e] = pack2<TYPE>(x, y);
+          l = add2<TYPE>(w[e], l);
+        }
       }
       p[k] = __builtin_bit_cast(s16x8, w);
     }
     // lane i of 16 points at 4 columns of key i / 4 and receives 4 keys of column i
     const int i = lane & 15, row = h * 4 + (i >> 2);
-    const uint32_t at = row * ROW + ((((lane >> 4) & 1) * 2 + ((i & 3) >> 1)) ^ S2::place(true, row)) * 16 + (i & 1) * 8;
+    const uint32_t at = row * ROW + ((((lane >> 4) & 1) * 2 + ((i & 3) >> 1)) ^ S2::v(row)) * 16 + (i & 1) * 8;
     auto values = [&](int t, int k) __attribute__((always_inline)) {
       const uint8_t* v0 = V + ((at ^ (t * 64)) + k * 16 * ROW);
       const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)v0), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(v0 + 8 * ROW));
@@ -495,14 +541,18 @@ struct Attention {
     begin();
     clear_lds();
     issue(it.b0, 0);
-    for (int b = it.b0; b < it.b1; ++b) {
-      const int stage = (b - it.b0) & 1;
-      settle(stage);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      lds_barrier();
-      if (b + 1 < it.b1) issue(b + 1, stage ^ 1);
-      compute(b, stage);
-    }
+    auto blocks = [&](auto rows) __attribute__((always_inline)) {
+      for (int b = it.b0; b < it.b1; ++b) {
+        const int stage = (b - it.b0) & 1;
+        settle(stage);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        if (b + 1 < it.b1) issue(b + 1, stage ^ 1);
+        if constexpr (decltype(rows)::value) compute(b, stage);
+      }
+    };
+    if (rows_here) blocks(std::true_type());
+    else blocks(std::false_type());                                // (a wave without rows brings its keys)
     l += other_half(l);
     if constexpr (FP8 && TYPE == kF16) {
 #pragma unroll
@@ -598,12 +648,15 @@ struct Attention {
     float lift = 1;
     clear_lds();
     uint32_t there[2];
+    Found place[2][N];
     auto issue_k = [&](int first, int turn) __attribute__((always_inline)) {
       need_pages(first, KT);
-      uint32_t on = 0;
 #pragma unroll
-      for (int n = 0; n < N; ++n) on |= bring<FP8 ? 1 : 2>(false, first + n * 16, lds_at(&sh.own[wave][turn][0][n * 16 * NROW])) << n * 16;
-      there[turn] = on;
+      for (int n = 0; n < N; ++n) {
+        place[turn][n] = find(first + n * 16);
+        bring<FP8 ? 1 : 2>(false, place[turn][n], n * 16, lds_at(&sh.own[wave][turn][0][n * 16 * NROW]));
+      }
+      there[turn] = N == 1 && place[turn][0].side_by_side ? 0xffffu : N == 2 && place[turn][0].side_by_side && place[turn][N - 1].side_by_side ? 0xffffffffu : which<KT>(first);
       if constexpr (FP8) {                                         // lanes 0 .. 31: scales of K, the others: of V
         int page, slot;
         const bool is = where(first + (lane & 31), page, slot);
@@ -611,10 +664,9 @@ struct Attention {
         load_lds4(is ? (const void*)from : (const void*)&kNothing, lds_at(&sh.scales[0][0][0]) + (wave * 2 + turn) * 256);
       }
     };
-    auto issue_v = [&](int first, int turn) __attribute__((always_inline)) {
-      need_pages(first, KT);                                       // (a key's pages are asked for again only if K has gone beyond them since)
+    auto issue_v = [&](int turn) __attribute__((always_inline)) {   // (of the keys whose K was issued last: their pages' entries are there)
 #pragma unroll
-      for (int n = 0; n < N; ++n) bring<FP8 ? 1 : 2>(true, first + n * 16, lds_at(&sh.own[wave][turn][1][n * 16 * NROW]));
+      for (int n = 0; n < N; ++n) bring<FP8 ? 1 : 2>(true, place[turn][n], n * 16, lds_at(&sh.own[wave][turn][1][n * 16 * NROW]));
     };
     auto body = [&](int first, int turn, int ahead) __attribute__((always_inline)) {
       const uint8_t *K = sh.own[wave][turn][0], *V = sh.own[wave][turn][1];
@@ -676,9 +728,8 @@ struct Attention {
         float top = fmaxf(fmaxf(s[x][0][0], s[x][0][1]), fmaxf(s[x][0][2], s[x][0][3]));
         if constexpr (N == 2) top = fmaxf(top, fmaxf(fmaxf(s[x][N - 1][0], s[x][N - 1][1]), fmaxf(s[x][N - 1][2], s[x][N - 1][3])));
         top = quarters<Max>(top) * a.scale_log2;
-        const float grown = fmaxf(mx[x], top);
-        if (__any(grown > mx[x])) {
-          const float by = grown > mx[x] ? exp2_fast(mx[x] - grown) : 1.0f;
+        if (__any(top > mx[x] + LAG)) {
+          const float grown = fmaxf(mx[x], top), by = grown > mx[x] ? exp2_fast(mx[x] - grown) : 1.0f;
           mx[x] = grown, ls[x] *= by;
 #pragma unroll
           for (int t = 0; t < DN; ++t) on[x][t] *= by;
@@ -687,10 +738,6 @@ struct Attention {
         float p[4 * N];
 #pragma unroll
         for (int e = 0; e < 4 * N; ++e) p[e] = exp2_fast(fmaf(s[x][e >> 2][e & 3], a.scale_log2, less));
-        if constexpr (!FP8) {
-#pragma unroll
-          for (int e = 0; e < 4 * N; ++e) ls[x] += p[e];
-        }
         u32x4 w = {};
         if constexpr (FP8) {
           const float by = 1.0f / lift;
@@ -702,7 +749,10 @@ struct Attention {
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; e += 2) w[e >> 1] = pack2<TYPE>(p[e], p[e + 1]);
+          for (int e = 0; e < 4; e += 2) {
+            w[e >> 1] = pack2<TYPE>(p[e], p[e + 1]);
+            ls[x] = add2<TYPE>(w[e >> 1], ls[x]);
+          }
         }
         pk[x] = __builtin_bit_cast(s16x8, w);
       }
@@ -723,10 +773,10 @@ struct Attention {
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      issue_v(ahead, turn);
+      issue_v(turn);
     };
     const int step = 4 * KT, first = k_begin + wave * KT;
-    issue_k(first, 0), issue_v(first, 0), issue_k(first + step, 1), issue_v(first + step, 1);
+    issue_k(first, 0), issue_v(0), issue_k(first + step, 1), issue_v(1);
     for (int at = k_begin; at < k_end; at += 2 * step) {
       body(at + wave * KT, 0, at + wave * KT + 2 * step);
       if (at + step < k_end) body(at + step + wave * KT, 1, at + wave * KT + 3 * step);
