@@ -335,11 +335,13 @@ struct Attention {
       return;
     }
     const bool any = f.first < it.keys.hi && f.first + 16 > it.keys.lo;
-    int page, slot;
-#pragma unroll
+    int ln = lane, page, slot;
+    asm volatile("" : "+v"(ln));                                   // (nothing of this is made ahead of the loop: it is rare, and the registers are needed)
+#pragma unroll 1
     for (int i = 0; i < S::NI; ++i) {
+      const int row = i * S::RPI + ln / S::CH, c = (ln % S::CH ^ S::place(v, row0 + row)) * 16;
       const void* from = &kNothing;
-      if (any && where(f.first + i * S::RPI + lane / S::CH, page, slot) && column(i) < a.D * EB) from = cache + (page * pl.page + slot * pl.slot) * EB + column(i);
+      if (any && where(f.first + row, page, slot) && c < a.D * EB) from = cache + (page * pl.page + slot * pl.slot) * EB + c;
       load_lds<false>(from, lds + i * 1024);
     }
   }
@@ -347,8 +349,9 @@ struct Attention {
   template <int KEYS>
   __device__ __forceinline__ uint32_t which(int first) {
     if (first >= it.keys.hi || first + KEYS <= it.keys.lo) return 0;
-    int page, slot;
-    return (uint32_t)__ballot(where(first + lane, page, slot) && lane < KEYS);
+    int ln = lane, page, slot;
+    asm volatile("" : "+v"(ln));
+    return (uint32_t)__ballot(where(first + ln, page, slot) && ln < KEYS);
   }
   // Columns from D to DP stay zero: nothing is loaded there.
   __device__ __forceinline__ void clear_lds() {
