@@ -921,6 +921,35 @@ struct Attention {
     work(0, -1, 0);
   }
 
+  // A place in the list of all blocks.
+  struct Spot {
+    Seq q;
+    Cost c;
+    int s, head, pair, at;                                         // block of the pair
+  };
+  __device__ __forceinline__ Spot spot(int64_t u, int s, int64_t before, int tokens) {
+    Spot p;
+    p.s = __builtin_amdgcn_readfirstlane(s);
+    p.q = sequence(a, p.s);
+    p.c = cost_of(a, p.q, tokens);
+    const int64_t of_head = (int64_t)p.c.pairs * p.c.cell;
+    int64_t rest = u - before;
+    p.head = __builtin_amdgcn_readfirstlane((int)(rest / of_head));
+    rest -= p.head * of_head;
+    p.pair = __builtin_amdgcn_readfirstlane((int)(rest / p.c.cell));
+    p.at = __builtin_amdgcn_readfirstlane((int)(rest - (int64_t)p.pair * p.c.cell));
+    return p;
+  }
+  // By how much a border there is moved.
+  __device__ __forceinline__ int64_t moved(const Spot& p, int tokens, int64_t near) {
+    const int tiles = tiles_of(a, p.q, tokens), last = tiles - 1 - p.pair;
+    const int n0 = tile_blocks(a, p.q, tokens, p.pair).count, n1 = last > p.pair ? tile_blocks(a, p.q, tokens, last).count : 0;
+    if (p.at <= near) return -p.at;
+    if (p.at - n0 <= near && n0 - p.at <= near) return n0 - p.at;
+    if (n0 + n1 - p.at <= near) return p.c.cell - p.at;
+    return 0;
+  }
+
   // A run of the list of all blocks.
   __device__ __forceinline__ void split() {
     const int tokens = ROWS / a.group.d, groups = a.groups;
@@ -945,40 +974,47 @@ struct Attention {
       if (threadIdx.x < 2 && !(wrote >> threadIdx.x & 1)) *(uint32_t*)(a.ws + part_at(a, group, threadIdx.x, DP)) = 0;
     };
     if (group >= busy) return done();
-    int64_t u = all * group / busy;
-    const int64_t end = all * (group + 1) / busy;
+    int64_t u = all * group / busy, end = all * (group + 1) / busy;
+    // A border near a tile's, by a thirtieth of a workgroup's share, is moved there, and the tile is not cut: a partial result costs more.  (Both sides of a border come to the same.)
+    const int64_t share = all / busy, near = share / 32 + 1;
+    const bool snap = share >= 8;
     for (int s = threadIdx.x; s < a.S; s += 256) {
-      const int64_t to = s + 1 < a.S ? before[s + 1] : carry;
-      if (before[s] * a.kv_heads <= u && u < to * a.kv_heads) sh.found[0] = s, sh.found[1] = before[s];
+      const int64_t from = before[s] * a.kv_heads, to = (s + 1 < a.S ? before[s + 1] : carry) * a.kv_heads;
+      if (from <= u && u < to) sh.found[0] = s, sh.found[1] = from;
+      if (from <= end && end < to) sh.found[2] = s, sh.found[3] = from;
     }
     lds_barrier();
-    int s = __builtin_amdgcn_readfirstlane((int)sh.found[0]);
-    int64_t rest = u - sh.found[1] * a.kv_heads;
+    Spot at = spot(u, (int)sh.found[0], sh.found[1], tokens);
+    if (snap && end < all) {
+      Spot e = spot(end, (int)sh.found[2], sh.found[3], tokens);
+      end += moved(e, tokens, near);
+    }
     lds_barrier();
-    it.s = s, it.q = sequence(a, s);
-    Cost c = cost_of(a, it.q, tokens);
-    int64_t of_head = (int64_t)c.pairs * c.cell;
-    it.head = __builtin_amdgcn_readfirstlane((int)(rest / of_head));
-    rest -= it.head * of_head;
-    int pair = __builtin_amdgcn_readfirstlane((int)(rest / c.cell)), at = __builtin_amdgcn_readfirstlane((int)(rest - (int64_t)pair * c.cell));
+    if (snap && u > 0) {
+      const int64_t by = moved(at, tokens, near);
+      u += by, at.at += (int)by;
+    }
+    it.s = at.s, it.q = at.q, it.head = at.head;
+    Cost c = at.c;
+    int pair = at.pair, in_pair = at.at;
     while (u < end) {
       const int tiles = tiles_of(a, it.q, tokens), lastt = tiles - 1 - pair;
       const int n0 = tile_blocks(a, it.q, tokens, pair).count, n1 = lastt > pair ? tile_blocks(a, it.q, tokens, lastt).count : 0;
-      if (at < n0 + n1) {
-        const bool second = at >= n0;
+      if (in_pair < n0 + n1) {
+        const bool second = in_pair >= n0;
         tile(second ? lastt : pair, tokens);
         const Blocks b = blocks_of(it.keys);
-        const int from = second ? at - n0 : at;
+        const int from = second ? in_pair - n0 : in_pair;
         const int64_t left = end - u;
         const int to = b.count - from <= left ? b.count : from + (int)left;
         it.b0 = b.first + from, it.b1 = b.first + to;
         const bool starts = from == 0, ends = to == b.count;
         work(group, starts && ends ? -1 : starts ? 1 : 0, ends);
         if (!(starts && ends)) wrote |= starts ? 2 : 1;
-        u += to - from, at += to - from;
+        u += to - from, in_pair += to - from;
       }
-      if (at >= n0 + n1) {                                         // the next pair, head, sequence
-        u += c.cell - at, at = 0;
+      if (in_pair >= n0 + n1) {                                         // the next pair, head, sequence
+        u += c.cell - in_pair, in_pair = 0;
         if (u >= end) break;
         if (++pair == c.pairs) {
           pair = 0;

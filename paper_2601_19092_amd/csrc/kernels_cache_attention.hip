@@ -5,76 +5,92 @@
 
 namespace axe {
 
-// Partial results of one tile: the workgroup that began it, then the workgroups behind it up to the one that ended it.  A wave joins a row: a lane a part for the maxima and sums, then
-// LANES lanes a part for the row itself, the parts' weights on the way, so that as many loads as possible are under way at once.
+// Partial results of one tile: those of the workgroup that began it, then of the workgroups behind it up to the one that ended it.  A wave joins RB rows at once; LANES lanes
+// have four columns each of a part's row and take every 64 / LANES-th part, DEPTH of them with their maxima and sums under way together.
+template <int TYPE, int DP>
+struct Join {
+  static constexpr int LANES = DP / 4, AT_ONCE = 64 / LANES;
+  const CacheArgs& a;
+  int group, n, token, kv_head, rows;                              // n parts
+  const int lane = threadIdx.x & 63;
+
+  template <int RB, int DEPTH>
+  __device__ __forceinline__ void run(int first, int step) const {
+    const int c = lane % LANES * 4;
+    for (int r0 = first; r0 < rows; r0 += RB * step) {
+      float top[RB], l[RB];
+      f32x4 o[RB];
+      int row[RB];
+#pragma unroll
+      for (int i = 0; i < RB; ++i) top[i] = -INFINITY, l[i] = 0, o[i] = f32x4{}, row[i] = r0 + i * step < rows ? r0 + i * step : rows - 1;
+      for (int j0 = lane / LANES; j0 < n; j0 += AT_ONCE * DEPTH) {
+        float pm[RB][DEPTH], pl[RB][DEPTH];
+        f32x4 v[RB][DEPTH];
+#pragma unroll
+        for (int k = 0; k < DEPTH; ++k) {
+          const int j = j0 + k * AT_ONCE, at = j < n ? j : n - 1;
+          const float* p = a.ws + part_at(a, group + at, at == 0, DP) + 4;
+#pragma unroll
+          for (int i = 0; i < RB; ++i) {
+            pm[i][k] = j < n ? p[row[i]] : -INFINITY, pl[i][k] = p[a.ws_rows + row[i]];
+            v[i][k] = *(const f32x4*)(p + 2 * a.ws_rows + (int64_t)row[i] * DP + c);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int k = 0; k < DEPTH; ++k) add(top[i], l[i], o[i], pm[i][k], pl[i][k], v[i][k]);
+      }
+#pragma unroll
+      for (int i = 0; i < RB; ++i) {
+        if constexpr (AT_ONCE >= 4) other<16>(top[i], l[i], o[i]);
+        if constexpr (AT_ONCE >= 2) other<32>(top[i], l[i], o[i]);
+        const float by = l[i] == 0 ? 0.0f : 1.0f / l[i];
+        const int t = (int)quotient(row[i], a.group), g = row[i] - t * (int)a.group.d;
+        uint16_t* to = (uint16_t*)a.out + (int64_t)(token + t) * a.os.token + (int64_t)(kv_head * (int)a.group.d + g) * a.os.head + c;
+        if (lane < LANES && c < a.D && r0 + i * step < rows) store_bits(to, u32x2{pack2<TYPE>(o[i][0] * by, o[i][1] * by), pack2<TYPE>(o[i][2] * by, o[i][3] * by)});
+      }
+    }
+  }
+  // Two results of one row (a maximum of -inf: no key was seen, and the rest is 0).
+  static __device__ __forceinline__ void add(float& top, float& l, f32x4& o, float pm, float pl, f32x4 v) {
+    const float t = fmaxf(top, pm), base = t == -INFINITY ? 0.0f : t, old = exp2_fast(top - base), by = exp2_fast(pm - base);
+    top = t, l = l * old, o = o * old;
+    if (pm != -INFINITY) l += pl * by, o += v * by;
+  }
+  template <int FAR>
+  static __device__ __forceinline__ void other(float& top, float& l, f32x4& o) {
+    auto far = [&](float x) __attribute__((always_inline)) { return __shfl_xor(x, FAR); };
+    const float pm = far(top), pl = far(l);
+    const f32x4 v = {far(o[0]), far(o[1]), far(o[2]), far(o[3])};
+    add(top, l, o, pm, pl, v);
+  }
+};
+
 template <int TYPE, int DP>
 __global__ __launch_bounds__(256) void cache_attention_join_kernel(CacheArgs a) {
-  constexpr int LANES = DP / 4, AT_ONCE = 64 / LANES, DEPTH = 8;   // a lane has four columns
   const int group = blockIdx.x, lane = threadIdx.x & 63;
   const uint32_t* head = (const uint32_t*)(a.ws + part_at(a, group, 1, DP));
-  const uint32_t valid = head[0];
-  const int token = (int)head[1], kv_head = (int)head[2], rows = (int)head[3];
-  int parts = 0;                                                   // behind the first
-  for (int g = group + 1; parts == g - group - 1; g += 64) {
+  const uint32_t begun = head[0];
+  int n = 1;
+  for (int g = group + 1;; g += 64) {                              // parts behind the first: up to the one that ends the tile
     const uint32_t flags = g + lane < a.groups ? *(const uint32_t*)(a.ws + part_at(a, g + lane, 0, DP)) : 0;
     const uint64_t none = __ballot(flags == 0), end = __ballot((flags & 2) != 0);
     const int until = none ? __ffsll((unsigned long long)none) - 1 : 64, last = end ? __ffsll((unsigned long long)end) : 64;
-    parts += until < last ? until : last;
-    if (until < 64 || last <= 64 && end) break;
+    n += until < last ? until : last;
+    if (none || end) break;
   }
-  if (!valid) return;
-  const int n = parts + 1;
-  auto part = [&](int i) __attribute__((always_inline)) { return a.ws + part_at(a, group + i, i == 0, DP); };
-  for (int r = blockIdx.y * 4 + (int)(threadIdx.x >> 6); r < rows; r += gridDim.y * 4) {
-    float top = -INFINITY;
-    for (int i = lane; i < n; i += 64) top = fmaxf(top, part(i)[4 + r]);
-    top = wave_all<Max>(top);
-    const float base = top == -INFINITY ? 0.0f : top;
-    float l = 0;
-    f32x4 o = {0, 0, 0, 0};
-    for (int i0 = 0; i0 < n; i0 += 64) {
-      const int mine = i0 + lane;
-      float by = 0;
-      if (mine < n) {
-        by = exp2_fast(part(mine)[4 + r] - base);
-        l += part(mine)[4 + a.ws_rows + r] * by;
-      }
-      const int many = n - i0 < 64 ? n - i0 : 64;
-      for (int j0 = 0; j0 < many; j0 += AT_ONCE * DEPTH) {
-        f32x4 v[DEPTH];
-#pragma unroll
-        for (int k = 0; k < DEPTH; ++k) {
-          const int j = j0 + k * AT_ONCE + lane / LANES;
-          v[k] = *(const f32x4*)(part(i0 + (j < many ? j : many - 1)) + 4 + 2 * a.ws_rows + (int64_t)r * DP + lane % LANES * 4);
-        }
-#pragma unroll
-        for (int k = 0; k < DEPTH; ++k) {
-          const int j = j0 + k * AT_ONCE + lane / LANES;
-          const float w = __shfl(by, j & 63);
-          if (j < many) o += v[k] * w;
-        }
-      }
-    }
-    l = wave_sum(l);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      if constexpr (AT_ONCE >= 2) o[c] += other_half(o[c]);
-      if constexpr (AT_ONCE >= 4) {
-        const auto x = __builtin_amdgcn_permlane16_swap(__float_as_int(o[c]), __float_as_int(o[c]), false, false);
-        o[c] = __int_as_float(x[0]) + __int_as_float(x[1]);
-      }
-    }
-    const float by = l == 0 ? 0.0f : 1.0f / l;
-    const int i = (int)quotient(r, a.group), g = r - i * (int)a.group.d, c = lane % LANES * 4;
-    uint16_t* to = (uint16_t*)a.out + (int64_t)(token + i) * a.os.token + (int64_t)(kv_head * (int)a.group.d + g) * a.os.head + c;
-    if (lane < LANES && c < a.D) store_bits(to, u32x2{pack2<TYPE>(o[0] * by, o[1] * by), pack2<TYPE>(o[2] * by, o[3] * by)});
-  }
+  if (!begun) return;
+  const Join<TYPE, DP> join{a, group, n, (int)head[1], (int)head[2], (int)head[3]};
+  const int first = blockIdx.y * 4 + (int)(threadIdx.x >> 6), step = gridDim.y * 4;
+  if (n <= 2 * Join<TYPE, DP>::AT_ONCE) join.template run<4, 2>(first, step);
+  else join.template run<1, 8>(first, step);
 }
 
 template <int TYPE>
 void launch_join(const CacheArgs& a, hipStream_t s) {
   const int dp = attn_columns(a.D);
-  const dim3 grid(a.groups, a.ws_rows <= 32 ? 4 : 16);
+  const dim3 grid(a.groups, a.ws_rows <= 32 ? 4 : 8);
   if (dp == 64) cache_attention_join_kernel<TYPE, 64><<<grid, 256, 0, s>>>(a);
   else if (dp == 128) cache_attention_join_kernel<TYPE, 128><<<grid, 256, 0, s>>>(a);
   else cache_attention_join_kernel<TYPE, 256><<<grid, 256, 0, s>>>(a);
