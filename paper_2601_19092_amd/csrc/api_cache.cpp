@@ -245,6 +245,7 @@ int axe_cache_attention(const axe_cache_desc_t* g, const void* d_q, const void* 
     a.causal = g->causal != 0, a.window = std::min<int64_t>(g->window, kMost);
     a.scale_log2 = (float)(g->scale * 1.4426950408889634);
     a.sixteens = g->page_tokens % 16 == 0 && std::max(p.kc.s[1], p.vc.s[1]) < (int64_t(1) << 26);
+    a.reach31 = !any || std::max((p.kc.mem.hi - p.kc.off) * cb, (p.vc.mem.hi - p.vc.off) * cb) < (int64_t(1) << 31) - 1024;
     a.groups = shape.groups, a.tile_rows = shape.tile_rows, a.ws_rows = shape.ws_rows;
     return finish(launch_cache_attention(a, (hipStream_t)stream), fn);
   });

@@ -262,6 +262,10 @@ struct Attention {
   };
   static_assert(4 * 2 * 2 * TURN <= 2 * 2 * BLOCK && sizeof(Shared::scales) == 4 * 2 * 64 * 4, "a turn of all waves is no more than a stage");
 
+  // Operands in LDS are read AHEAD of the product that takes them, which the compiler would not do: it reads, waits, multiplies.  Hence steps that stay in the order written.
+  static constexpr int AHEAD = 4;
+  static __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
   const CacheArgs& a;
   Shared& sh;
   const int lane, wave, h;
@@ -334,8 +338,22 @@ struct Attention {
       }
       return;
     }
-    const bool any = f.first < it.keys.hi && f.first + 16 > it.keys.lo;
     int ln = lane, page, slot;
+    if (a.reach31 && f.first >= it.keys.lo && f.first + 16 <= it.keys.hi) {   // all there, in pages of their own, and 32 bits hold the way to each: a lane works it out for each key
+      asm volatile("" : "+v"(ln));
+      const bool on = where(f.first + (ln & 15), page, slot);
+      if (__all(on)) {
+        const uint32_t at = (uint32_t)page * (uint32_t)(pl.page * EB) + (uint32_t)slot * (uint32_t)(pl.slot * EB);
+#pragma unroll
+        for (int i = 0; i < S::NI; ++i) {
+          const int row = i * S::RPI + ln / S::CH, c = (ln % S::CH ^ S::place(v, row0 + row)) * 16;
+          const uint32_t off = (uint32_t)__shfl((int)at, row) + c;
+          if (c < a.D * EB) load_lds<ONCE>(off, cache, lds + i * 1024);
+        }
+        return;
+      }
+    }
+    const bool any = f.first < it.keys.hi && f.first + 16 > it.keys.lo;
     asm volatile("" : "+v"(ln));                                   // (nothing of this is made ahead of the loop: it is rare, and the registers are needed)
 #pragma unroll 1
     for (int i = 0; i < S::NI; ++i) {
@@ -427,6 +445,8 @@ struct Attention {
       q[k] = s16x8{};
       if (on && c < a.D) q[k] = __builtin_bit_cast(s16x8, load_bits<u32x4>(from + c));
     }
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) asm volatile("" : "+v"(q[k])); // (waited for here: where they are used a wait would be one for the keys on their way)
     const Range mine = seen(a, it.q, it.i0 + i, it.i0 + i);
     lo = mine.lo, hi = mine.hi;
     const int last = rows - 1 < wave * 32 + 31 ? rows - 1 : wave * 32 + 31;
@@ -447,10 +467,16 @@ struct Attention {
     f32x16 s[2] = {f32x16{}, f32x16{}};
     {
       const uint32_t at = (lane & 31) * ROW + (h ^ S2::k(lane & 31)) * 16;
+      auto read = [&](int i) __attribute__((always_inline)) { return *(const s16x8*)(K + ((at ^ ((i >> 1) * 32)) + (i & 1) * 32 * ROW)); };
+      s16x8 k[AHEAD];
 #pragma unroll
-      for (int k = 0; k < STEPS; ++k) {
+      for (int i = 0; i < AHEAD; ++i) k[i] = read(i);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) s[t] = mfma32<TYPE>(*(const s16x8*)(K + ((at ^ (k * 32)) + t * 32 * ROW)), q[k], s[t]);
+      for (int i = 0; i < STEPS * 2; ++i) {
+        const s16x8 now = k[i % AHEAD];
+        in_order();
+        if (i + AHEAD < STEPS * 2) k[i % AHEAD] = read(i + AHEAD);
+        s[i & 1] = mfma32<TYPE>(now, q[i >> 1], s[i & 1]);
       }
     }
     if constexpr (FP8) {
@@ -488,10 +514,6 @@ struct Attention {
         for (int r = 0; r < 16; ++r) o[t][r] *= by;
     }
     const float less = LIFT - (m == -INFINITY ? 0.0f : m);
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[t][r] = exp2_fast(fmaf(s[t][r], a.scale_log2, less));
     float by_v = 1;
     if constexpr (FP8 && TYPE == kF16) {                           // as in run_narrow
       const float sv = sh.scales[stage][1][lane], most = wave_all<Max>(fabsf(sv) <= 3.0e38f ? fabsf(sv) : 0.0f);
@@ -505,38 +527,47 @@ struct Attention {
       }
       by_v = 1.0f / lift_v;
     }
-    s16x8 p[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = (k & 1) * 8 + 2 * e;
-        const float x = s[k >> 1][r], y = s[k >> 1][r + 1];
-        if constexpr (FP8) {
-          const float* sc = &sh.scales[stage][1][k * 16 + (e >> 1) * 8 + h * 4 + (e & 1) * 2];
-          const float v0 = sc[0] * by_v, v1 = sc[1] * by_v, t0 = x * v0, t1 = y * v1;
-          w[e] = pack2<TYPE>(t0, t1);
-          l += weight(x, t0, v0, half<TYPE>(w[e], 0)) + weight(y, t1, v1, half<TYPE>(w[e], 1));
-        } else {
-          w[e] = pack2<TYPE>(x, y);
-          l = add2<TYPE>(w[e], l);
-        }
-      }
-      p[k] = __builtin_bit_cast(s16x8, w);
-    }
     // lane i of 16 points at 4 columns of key i / 4 and receives 4 keys of column i
     const int i = lane & 15, row = h * 4 + (i >> 2);
     const uint32_t at = row * ROW + ((((lane >> 4) & 1) * 2 + ((i & 3) >> 1)) ^ S2::v(row)) * 16 + (i & 1) * 8;
-    auto values = [&](int t, int k) __attribute__((always_inline)) {
-      const uint8_t* v0 = V + ((at ^ (t * 64)) + k * 16 * ROW);
+    auto read = [&](int i) __attribute__((always_inline)) {        // of keys 16 (i / DT) .., columns 32 (i mod DT) ..
+      const uint8_t* v0 = V + ((at ^ (i % DT * 64)) + i / DT * 16 * ROW);
       const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)v0), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(v0 + 8 * ROW));
       return s16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     };
+    // Two terms of 16 keys k: p[k], pair e of four.
+    u32x4 p[4];
+    auto two = [&](int k, int e) __attribute__((always_inline)) {
+      const int r = (k & 1) * 8 + 2 * e;
+      const float x = exp2_fast(fmaf(s[k >> 1][r], a.scale_log2, less)), y = exp2_fast(fmaf(s[k >> 1][r + 1], a.scale_log2, less));
+      if constexpr (FP8) {
+        const float* sc = &sh.scales[stage][1][k * 16 + (e >> 1) * 8 + h * 4 + (e & 1) * 2];
+        const float v0 = sc[0] * by_v, v1 = sc[1] * by_v, t0 = x * v0, t1 = y * v1;
+        p[k][e] = pack2<TYPE>(t0, t1);
+        l += weight(x, t0, v0, half<TYPE>(p[k][e], 0)) + weight(y, t1, v1, half<TYPE>(p[k][e], 1));
+      } else {
+        p[k][e] = pack2<TYPE>(x, y);
+        l = add2<TYPE>(p[k][e], l);
+      }
+    };
+    // The terms of 16 keys, and their product with V: the next 16 keys' terms keep the vector unit while this product keeps the matrix unit.
+    s16x8 v[AHEAD];
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+    for (int i = 0; i < AHEAD; ++i) v[i] = read(i);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[t] = mfma32<TYPE>(values(t, k), p[k], o[t]);
+    for (int e = 0; e < 4; ++e) two(0, e);
+#pragma unroll
+    for (int i = 0; i < DT * 4; ++i) {
+      const s16x8 now = v[i % AHEAD];
+      in_order();
+      if (i + AHEAD < DT * 4) v[i % AHEAD] = read(i + AHEAD);
+      o[i % DT] = mfma32<TYPE>(now, __builtin_bit_cast(s16x8, p[i / DT]), o[i % DT]);
+      if (i / DT < 3) {
+#pragma unroll
+        for (int e = 4 * (i % DT) / DT; e < 4 * (i % DT + 1) / DT; ++e) two(i / DT + 1, e);
+      }
+    }
+    in_order();
   }
 
   // All blocks of the item, for the rows of all waves.
@@ -640,6 +671,8 @@ struct Attention {
         qn[x][k] = s16x8{};
         if (r < rows && c < a.D) qn[x][k] = __builtin_bit_cast(s16x8, load_bits<u32x4>(from + c));
       }
+#pragma unroll
+      for (int k = 0; k < SN32; ++k) asm volatile("" : "+v"(qn[x][k]));   // (as in begin)
       const Range mine = seen(a, it.q, it.i0 + i, it.i0 + i);
       rlo[x] = mine.lo, rhi[x] = mine.hi;
       mx[x] = -INFINITY, ls[x] = 0;
@@ -968,16 +1001,18 @@ struct Attention {
     }
     lds_barrier();
     const int64_t all = carry * a.kv_heads;
-    const int64_t busy = all < groups ? all : groups;              // (each of them has a block at least: parts of a tile lie in neighbouring workgroups' places)
+    // Each of them has a block at least (parts of a tile lie in neighbouring workgroups' places); of wide tiles four, where that makes 128 of them: a partial result takes as long as a block or two.
+    int64_t busy = RT || all < 512 ? all : all / 4;
+    busy = RT == 0 && all < 512 && busy > 128 ? 128 : busy < groups ? busy : groups;
     int wrote = 0;                                                 // parts
     auto done = [&]() __attribute__((always_inline)) {
       if (threadIdx.x < 2 && !(wrote >> threadIdx.x & 1)) *(uint32_t*)(a.ws + part_at(a, group, threadIdx.x, DP)) = 0;
     };
     if (group >= busy) return done();
     int64_t u = all * group / busy, end = all * (group + 1) / busy;
-    // A border near a tile's, by a thirtieth of a workgroup's share, is moved there, and the tile is not cut: a partial result costs more.  (Both sides of a border come to the same.)
-    const int64_t share = all / busy, near = share / 32 + 1;
-    const bool snap = share >= 8;
+    // Wide tiles: a border near a tile's is moved there, and the tile is not cut.  (Both sides of a border come to the same.)
+    const int64_t share = all / busy, near = share / 32 + 1 + (share >= 16);
+    const bool snap = RT == 0 && share >= 8;
     for (int s = threadIdx.x; s < a.S; s += 256) {
       const int64_t from = before[s] * a.kv_heads, to = (s + 1 < a.S ? before[s + 1] : carry) * a.kv_heads;
       if (from <= u && u < to) sh.found[0] = s, sh.found[1] = from;

@@ -42,6 +42,7 @@ struct CacheArgs {
   float scale_log2;                // scale / ln 2
   int32_t type, fp8;               // kBf16 or kF16; e4m3 cache
   int32_t sixteens;                // attention: 16 keys from a multiple of 16 on lie in one page, within 2^31 bytes of each other
+  int32_t reach31;                 // attention: both caches' elements lie within 2^31 bytes
   int32_t groups;                  // attention, split form: workgroups
   int32_t tile_rows;               // 16, 32 or kAttnRows
   int32_t ws_rows;                 // rows of a partial result

@@ -83,7 +83,7 @@ __global__ __launch_bounds__(256) void cache_attention_join_kernel(CacheArgs a) 
   if (!begun) return;
   const Join<TYPE, DP> join{a, group, n, (int)head[1], (int)head[2], (int)head[3]};
   const int first = blockIdx.y * 4 + (int)(threadIdx.x >> 6), step = gridDim.y * 4;
-  if (n <= 2 * Join<TYPE, DP>::AT_ONCE) join.template run<4, 2>(first, step);
+  if (join.rows > 16) join.template run<4, 4>(first, step);
   else join.template run<1, 8>(first, step);
 }
 
