@@ -289,6 +289,14 @@ struct Attention {
     entries = p0 + lane < a.max_pages ? a.table[(int64_t)it.s * a.max_pages + p0 + lane] : -1;
     asm volatile("" : "+v"(entries));                              // (waited for here, where it is rare: the loads into LDS would be waited for too)
   }
+  // The same before an item's first keys, not waited for: the queries come with them.
+  __device__ __forceinline__ void first_pages(int first) {
+    const int from = first > it.keys.lo ? first : it.keys.lo;
+    page0 = -1000, entries = -1;
+    if (from >= it.keys.hi) return;
+    page0 = (int)quotient(from, a.page);
+    if (page0 + lane < a.max_pages) entries = a.table[(int64_t)it.s * a.max_pages + page0 + lane];
+  }
   // Whether sixteen keys from `first`, a multiple of 16, on all are there, side by side in one page; then where they begin.
   __device__ __forceinline__ bool together(int first, int& page, int& slot) {
     if (!a.sixteens || first < it.keys.lo || first + 16 > it.keys.hi) return false;
@@ -445,6 +453,7 @@ struct Attention {
       q[k] = s16x8{};
       if (on && c < a.D) q[k] = __builtin_bit_cast(s16x8, load_bits<u32x4>(from + c));
     }
+    asm volatile("" : "+v"(entries));
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) asm volatile("" : "+v"(q[k])); // (waited for here: where they are used a wait would be one for the keys on their way)
     const Range mine = seen(a, it.q, it.i0 + i, it.i0 + i);
@@ -572,6 +581,7 @@ struct Attention {
 
   // All blocks of the item, for the rows of all waves.
   __device__ __forceinline__ void run_wide() {
+    first_pages(it.b0 * kAttnKeys + wave * 16);
     begin();
     clear_lds();
     issue(it.b0, 0);
@@ -657,6 +667,7 @@ struct Attention {
     keys.lo = keys.lo > k_begin ? keys.lo : k_begin, keys.hi = keys.hi < k_end ? keys.hi : k_end;
     const Range all = it.keys;
     it.keys = keys;
+    first_pages(k_begin + wave * KT);
     s16x8 qn[RT][SN32];
     int rlo[RT], rhi[RT];
     float mx[RT], ls[RT];
@@ -671,8 +682,13 @@ struct Attention {
         qn[x][k] = s16x8{};
         if (r < rows && c < a.D) qn[x][k] = __builtin_bit_cast(s16x8, load_bits<u32x4>(from + c));
       }
+      if (x == RT - 1) {
+        asm volatile("" : "+v"(entries));
 #pragma unroll
-      for (int k = 0; k < SN32; ++k) asm volatile("" : "+v"(qn[x][k]));   // (as in begin)
+        for (int y = 0; y < RT; ++y)
+#pragma unroll
+          for (int k = 0; k < SN32; ++k) asm volatile("" : "+v"(qn[y][k]));   // (as in begin)
+      }
       const Range mine = seen(a, it.q, it.i0 + i, it.i0 + i);
       rlo[x] = mine.lo, rhi[x] = mine.hi;
       mx[x] = -INFINITY, ls[x] = 0;
@@ -714,17 +730,27 @@ struct Attention {
       for (int x = 0; x < RT; ++x)
 #pragma unroll
         for (int n = 0; n < N; ++n) s[x][n] = f32x4{};
+      {
+        using Raw = std::conditional_t<FP8, u32x2, u32x4>;
+        auto read = [&](int i) __attribute__((always_inline)) {
+          const int row = i / SN32 * 16 + col;
+          if constexpr (FP8) return *(const u32x2*)(K + ((row * NROW + ((kg >> 1) ^ SN::k(row)) * 16 + (kg & 1) * 8) ^ (i % SN32 * 32)));
+          else return *(const u32x4*)(K + ((row * NROW + (kg ^ SN::k(row)) * 16) ^ (i % SN32 * 64)));
+        };
+        Raw k[AHEAD];
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+        for (int i = 0; i < AHEAD && i < N * SN32; ++i) k[i] = read(i);
 #pragma unroll
-        for (int k = 0; k < SN32; ++k) {
-          const int row = n * 16 + col;
-          s16x8 kf;
-          if constexpr (FP8) kf = widen<TYPE>(*(const u32x2*)(K + ((row * NROW + ((kg >> 1) ^ SN::place(false, row)) * 16 + (kg & 1) * 8) ^ (k * 32))));
-          else kf = *(const s16x8*)(K + ((row * NROW + (kg ^ SN::place(false, row)) * 16) ^ (k * 64)));
+        for (int i = 0; i < N * SN32; ++i) {
+          s16x8 now;
+          if constexpr (FP8) now = widen<TYPE>(k[i % AHEAD]);
+          else now = __builtin_bit_cast(s16x8, k[i % AHEAD]);
+          in_order();
+          if (i + AHEAD < N * SN32) k[i % AHEAD] = read(i + AHEAD);
 #pragma unroll
-          for (int x = 0; x < RT; ++x) s[x][n] = mfma16<TYPE>(kf, qn[x][k], s[x][n]);
+          for (int x = 0; x < RT; ++x) s[x][i / SN32] = mfma16<TYPE>(now, qn[x][i % SN32], s[x][i / SN32]);
         }
+      }
       f32x4 vs[N];
       if constexpr (FP8) {
 #pragma unroll
@@ -793,19 +819,33 @@ struct Attention {
         pk[x] = __builtin_bit_cast(s16x8, w);
       }
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LK + LV) : "memory");
+      {
+        using Raw = std::conditional_t<FP8, i32x2, s16x4>;
+        auto read = [&](int t) __attribute__((always_inline)) {
+          if constexpr (FP8) {
+            const int j = col >> 1, row = 16 * (j >> 2) + 4 * kg + (j & 3);
+            return __builtin_amdgcn_ds_read_tr8_b64_v2i32((tr8_ptr)(V + ((row * NROW + SN::v(row) * 16 + (col & 1) * 8) ^ (t * 16))));
+          } else {
+            const int row = 4 * kg + (col >> 2);
+            return __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(V + ((row * NROW + (((col & 3) >> 1) ^ SN::v(row)) * 16 + (col & 1) * 8) ^ (t * 32))));
+          }
+        };
+        Raw v[AHEAD];
 #pragma unroll
-      for (int t = 0; t < DN; ++t) {
-        if constexpr (FP8) {
-          const int j = col >> 1, row = 16 * (j >> 2) + 4 * kg + (j & 3);
-          const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((tr8_ptr)(V + ((row * NROW + SN::place(true, row) * 16 + (col & 1) * 8) ^ (t * 16))));
-          const s16x8 vf = widen<TYPE>(u32x2{(uint32_t)v[0], (uint32_t)v[1]});
+        for (int t = 0; t < AHEAD; ++t) v[t] = read(t);
 #pragma unroll
-          for (int x = 0; x < RT; ++x) on[x][t] = mfma16<TYPE>(vf, pk[x], on[x][t]);
-        } else {
-          const int row = 4 * kg + (col >> 2);
-          const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(V + ((row * NROW + (((col & 3) >> 1) ^ SN::place(true, row)) * 16 + (col & 1) * 8) ^ (t * 32))));
+        for (int t = 0; t < DN; ++t) {
+          const Raw raw = v[t % AHEAD];
+          in_order();
+          if (t + AHEAD < DN) v[t % AHEAD] = read(t + AHEAD);
+          if constexpr (FP8) {
+            const s16x8 now = widen<TYPE>(u32x2{(uint32_t)raw[0], (uint32_t)raw[1]});
 #pragma unroll
-          for (int x = 0; x < RT; ++x) on[x][t] = mfma16_short<TYPE>(v, s16x4{pk[x][0], pk[x][1], pk[x][2], pk[x][3]}, on[x][t]);
+            for (int x = 0; x < RT; ++x) on[x][t] = mfma16<TYPE>(now, pk[x], on[x][t]);
+          } else {
+#pragma unroll
+            for (int x = 0; x < RT; ++x) on[x][t] = mfma16_short<TYPE>(raw, s16x4{pk[x][0], pk[x][1], pk[x][2], pk[x][3]}, on[x][t]);
+          }
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -888,7 +928,6 @@ struct Attention {
       const bool check = i < 0 && a.causal && tokens > 1;
       const int skip = i < 0 ? 0 : i;
       bool again = false;
-      page0 = -1000;
       if constexpr (RT > 0) run_narrow(group, part, ends, skip, tokens, check, again);
       else {
         run_wide();
@@ -932,27 +971,48 @@ struct Attention {
     const int tokens = ROWS / a.group.d;
     const int64_t number = a.t0 + blockIdx.x, want = number / a.kv_heads;
     it.head = (int)(number - want * a.kv_heads);
-    int64_t carry = 0;
-    if (threadIdx.x == 0) sh.found[0] = -1;
-    for (int base = 0; base < a.S; base += 256) {                  // sequences from the last on
-      const int s = a.S - 1 - base - (int)threadIdx.x;
-      const int n = s >= 0 ? tiles_of(a, sequence(a, s), tokens) : 0;
-      int64_t total;
-      const int64_t before = carry + scan(n, total);
-      if (want >= before && want < before + n) sh.found[0] = s, sh.found[1] = n - 1 - (want - before);
-      carry += total;
+    int t;
+    if (a.S <= 64) {                                               // a lane each, in every wave
+      Seq mine = {0, 0, 0, 0};
+      if (lane < a.S) mine = sequence(a, lane);
+      const int n = tiles_of(a, mine, tokens);
+      int upto = n;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int y = __shfl_up(upto, d);
+        if (lane >= d) upto += y;
+      }
+      const int64_t at = __builtin_amdgcn_readlane(upto, 63) - 1 - want;
+      if (at < 0) return;
+      upto -= n;
+      it.s = __popcll(__ballot(lane < a.S && upto <= at)) - 1;     // (the last that begins there or before: it has tiles)
+      it.q = {__builtin_amdgcn_readlane(mine.row0, it.s), __builtin_amdgcn_readlane(mine.n, it.s), __builtin_amdgcn_readlane(mine.first, it.s), __builtin_amdgcn_readlane(mine.len, it.s)};
+      t = (int)at - __builtin_amdgcn_readlane(upto, it.s);
+    } else {
+      int64_t carry = 0;
+      if (threadIdx.x == 0) sh.found[0] = -1;
+      for (int base = 0; base < a.S; base += 256) {                // sequences from the last on
+        const int s = a.S - 1 - base - (int)threadIdx.x;
+        const int n = s >= 0 ? tiles_of(a, sequence(a, s), tokens) : 0;
+        int64_t total;
+        const int64_t before = carry + scan(n, total);
+        if (want >= before && want < before + n) sh.found[0] = s, sh.found[1] = n - 1 - (want - before);
+        carry += total;
+        lds_barrier();
+        if (want < carry) break;
+      }
       lds_barrier();
-      if (want < carry) break;
+      it.s = __builtin_amdgcn_readfirstlane((int)sh.found[0]), t = __builtin_amdgcn_readfirstlane((int)sh.found[1]);
+      if (it.s < 0) return;
+      it.q = sequence(a, it.s);
     }
-    const int s = __builtin_amdgcn_readfirstlane((int)sh.found[0]), t = __builtin_amdgcn_readfirstlane((int)sh.found[1]);
-    if (s < 0) return;
-    it.s = s;
-    it.q = sequence(a, s);
     tile(t, tokens);
     const Blocks b = blocks_of(it.keys);
     it.b0 = b.first, it.b1 = b.first + b.count;
     work(0, -1, 0);
   }
+
+  static __device__ __forceinline__ int64_t over(int64_t x, int64_t y) { return (x | y) >> 31 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y); }   // (not negative)
 
   // A place in the list of all blocks.
   struct Spot {
@@ -960,16 +1020,16 @@ struct Attention {
     Cost c;
     int s, head, pair, at;                                         // block of the pair
   };
-  __device__ __forceinline__ Spot spot(int64_t u, int s, int64_t before, int tokens) {
+  __device__ __forceinline__ Spot spot(int64_t u, int s, const Seq& q, int64_t before, int tokens) {
     Spot p;
     p.s = __builtin_amdgcn_readfirstlane(s);
-    p.q = sequence(a, p.s);
+    p.q = q;
     p.c = cost_of(a, p.q, tokens);
     const int64_t of_head = (int64_t)p.c.pairs * p.c.cell;
     int64_t rest = u - before;
-    p.head = __builtin_amdgcn_readfirstlane((int)(rest / of_head));
+    p.head = __builtin_amdgcn_readfirstlane((int)over(rest, of_head));
     rest -= p.head * of_head;
-    p.pair = __builtin_amdgcn_readfirstlane((int)(rest / p.c.cell));
+    p.pair = __builtin_amdgcn_readfirstlane((int)over(rest, p.c.cell));
     p.at = __builtin_amdgcn_readfirstlane((int)(rest - (int64_t)p.pair * p.c.cell));
     return p;
   }
@@ -990,16 +1050,36 @@ struct Attention {
     const int group = (int)(blockIdx.x & 7) * (groups >> 3) + (int)(blockIdx.x >> 3);
     int64_t* before = (int64_t*)&sh.kv[0][0][0];                   // of the sequences, in blocks of one head
     int64_t carry = 0;
-    for (int base = 0; base < a.S; base += 256) {
-      const int s = base + (int)threadIdx.x;
+    // Up to 64 sequences: a lane each, in every wave.
+    Seq mine = {0, 0, 0, 0};
+    int upto = 0;
+    bool few = a.S <= 64;
+    if (few) {
       Cost c = {0, 0};
-      if (s < a.S) c = cost_of(a, sequence(a, s), tokens);
-      int64_t total;
-      const int64_t at = scan((int64_t)c.pairs * c.cell, total);
-      if (s < a.S) before[s] = carry + at;
-      carry += total;
+      if (lane < a.S) mine = sequence(a, lane), c = cost_of(a, mine, tokens);
+      const int64_t v = (int64_t)c.pairs * c.cell;
+      few = !__any(v >> 24);
+      upto = (int)v;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int y = __shfl_up(upto, d);
+        if (lane >= d) upto += y;
+      }
+      carry = few ? __builtin_amdgcn_readlane(upto, 63) : 0;
+      upto -= (int)v;                                              // before this lane's
     }
-    lds_barrier();
+    if (!few) {
+      for (int base = 0; base < a.S; base += 256) {
+        const int s = base + (int)threadIdx.x;
+        Cost c = {0, 0};
+        if (s < a.S) c = cost_of(a, sequence(a, s), tokens);
+        int64_t total;
+        const int64_t at = scan((int64_t)c.pairs * c.cell, total);
+        if (s < a.S) before[s] = carry + at;
+        carry += total;
+      }
+      lds_barrier();
+    }
     const int64_t all = carry * a.kv_heads;
     // Each of them has a block at least (parts of a tile lie in neighbouring workgroups' places); of wide tiles four, where that makes 128 of them: a partial result takes as long as a block or two.
     int64_t busy = RT || all < 512 ? all : all / 4;
@@ -1009,22 +1089,35 @@ struct Attention {
       if (threadIdx.x < 2 && !(wrote >> threadIdx.x & 1)) *(uint32_t*)(a.ws + part_at(a, group, threadIdx.x, DP)) = 0;
     };
     if (group >= busy) return done();
-    int64_t u = all * group / busy, end = all * (group + 1) / busy;
+    int64_t u = over(all * group, busy), end = over(all * (group + 1), busy);
     // Wide tiles: a border near a tile's is moved there, and the tile is not cut.  (Both sides of a border come to the same.)
-    const int64_t share = all / busy, near = share / 32 + 1 + (share >= 16);
+    const int64_t share = over(all, busy), near = share / 32 + 1 + (share >= 16);
     const bool snap = RT == 0 && share >= 8;
-    for (int s = threadIdx.x; s < a.S; s += 256) {
-      const int64_t from = before[s] * a.kv_heads, to = (s + 1 < a.S ? before[s + 1] : carry) * a.kv_heads;
-      if (from <= u && u < to) sh.found[0] = s, sh.found[1] = from;
-      if (from <= end && end < to) sh.found[2] = s, sh.found[3] = from;
+    Spot at, e;
+    if (few) {
+      auto find = [&](int64_t where) __attribute__((always_inline)) {
+        const int s = __popcll(__ballot(lane < a.S && (int64_t)upto * a.kv_heads <= where)) - 1;   // (the last that begins there or before: it has blocks, or `where` is the end)
+        const Seq q = {__builtin_amdgcn_readlane(mine.row0, s), __builtin_amdgcn_readlane(mine.n, s), __builtin_amdgcn_readlane(mine.first, s), __builtin_amdgcn_readlane(mine.len, s)};
+        return spot(where, s, q, (int64_t)__builtin_amdgcn_readlane(upto, s) * a.kv_heads, tokens);
+      };
+      at = find(u);
+      if (snap && end < all) e = find(end);
+    } else {
+      for (int s = threadIdx.x; s < a.S; s += 256) {
+        const int64_t from = before[s] * a.kv_heads, to = (s + 1 < a.S ? before[s + 1] : carry) * a.kv_heads;
+        if (from <= u && u < to) sh.found[0] = s, sh.found[1] = from;
+        if (from <= end && end < to) sh.found[2] = s, sh.found[3] = from;
+      }
+      lds_barrier();
+      auto find = [&](int64_t where, int k) __attribute__((always_inline)) {
+        const int s = __builtin_amdgcn_readfirstlane((int)sh.found[k]);
+        return spot(where, s, sequence(a, s), sh.found[k + 1], tokens);
+      };
+      at = find(u, 0);
+      if (snap && end < all) e = find(end, 2);
+      lds_barrier();
     }
-    lds_barrier();
-    Spot at = spot(u, (int)sh.found[0], sh.found[1], tokens);
-    if (snap && end < all) {
-      Spot e = spot(end, (int)sh.found[2], sh.found[3], tokens);
-      end += moved(e, tokens, near);
-    }
-    lds_barrier();
+    if (snap && end < all) end += moved(e, tokens, near);
     if (snap && u > 0) {
       const int64_t by = moved(at, tokens, near);
       u += by, at.at += (int)by;
@@ -1072,6 +1165,7 @@ template <int TYPE, bool FP8, int DP, int RT, bool SPLIT>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void cache_attention_kernel(CacheArgs a) {
   using A = Attention<TYPE, FP8, DP, RT>;
   __shared__ typename A::Shared sh;
+  fetch_arguments(a.q, a.k_scales, a.qs.token, a.kp.page, a.T, a.S, a.page.by.mul, a.type);
   A w(a, sh);
   if constexpr (SPLIT) w.split();
   else w.whole_tiles();

@@ -51,11 +51,11 @@ hipError_t launch_cache_append(const CacheArgs& a, hipStream_t s);
 hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t s);
 
 template <int RT>
-void launch_attention_narrow(const CacheArgs& a, hipStream_t s);
+void launch_attention_narrow(const CacheArgs& a, uint32_t groups, hipStream_t s);   // groups: workgroups (a.groups in the split form)
 template <>
-void launch_attention_narrow<1>(const CacheArgs& a, hipStream_t s);
+void launch_attention_narrow<1>(const CacheArgs& a, uint32_t groups, hipStream_t s);
 template <>
-void launch_attention_narrow<2>(const CacheArgs& a, hipStream_t s);
+void launch_attention_narrow<2>(const CacheArgs& a, uint32_t groups, hipStream_t s);
 
 // ---- attention: the shape of a call
 
@@ -63,23 +63,26 @@ constexpr int kAttnRows = 128;     // rows (tokens x query heads of one head of 
 constexpr int kAttnKeys = 64;      // keys of a block
 constexpr int kAttnMaxGroup = 128; // query heads of a head of the cache
 constexpr int kAttnSplitSeqs = 4096;
+constexpr int kAttnFewKeys = 256;
 
 inline int attn_columns(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 // Workgroups that the chip holds at once.
 inline int attn_slots(int D) { return attn_columns(D) <= 128 ? 512 : 256; }
 
-// groups: workgroups of the split form, 0: every tile a workgroup's.  The keys of a tile are split among workgroups unless there are tiles enough to fill the chip some times over.
+// groups: workgroups of the split form, 0: every tile a workgroup's.  The keys of a tile are split among workgroups unless there are tiles enough to fill the chip some times over, or so few
+// keys (of narrow tiles) that the second launch takes longer.
 // Rows of a tile: as many as the sequences have on average, up to 32; from there on 128.
 struct AttnShape {
   int tile_rows, groups, ws_rows;
 };
-inline AttnShape attn_shape(int64_t T, int S, int kv_heads, int group, int D) {
+inline AttnShape attn_shape(int64_t T, int S, int kv_heads, int group, int D, int64_t capacity) {
   AttnShape r = {kAttnRows, 0, 0};
   if (T == 0 || S == 0) return r;
   const int64_t wide = kAttnRows / group, tiles = (T + wide - 1) / wide * kv_heads;
   if (S > kAttnSplitSeqs || tiles >= 2 * (int64_t)attn_slots(D)) return r;
   const int64_t rows = (T + S - 1) / S * group;
   if (rows <= 32) r.tile_rows = rows <= 16 ? 16 : 32;
+  if (r.tile_rows <= 32 && capacity <= kAttnFewKeys) return r;
   r.groups = attn_slots(D);
   const int64_t tokens = r.tile_rows / group, most = T < tokens ? T * group : r.tile_rows;
   r.ws_rows = (int)((most + 15) / 16 * 16);

@@ -83,8 +83,11 @@ __global__ __launch_bounds__(256) void cache_attention_join_kernel(CacheArgs a) 
   if (!begun) return;
   const Join<TYPE, DP> join{a, group, n, (int)head[1], (int)head[2], (int)head[3]};
   const int first = blockIdx.y * 4 + (int)(threadIdx.x >> 6), step = gridDim.y * 4;
-  if (join.rows > 16) join.template run<4, 4>(first, step);
-  else join.template run<1, 8>(first, step);
+  constexpr int AT_ONCE = Join<TYPE, DP>::AT_ONCE;
+  if (join.rows <= 16) join.template run<1, 8>(first, step);
+  else if (n <= AT_ONCE) join.template run<4, 1>(first, step);
+  else if (n <= 2 * AT_ONCE) join.template run<4, 2>(first, step);
+  else join.template run<4, 4>(first, step);
 }
 
 template <int TYPE>
@@ -98,17 +101,22 @@ void launch_join(const CacheArgs& a, hipStream_t s) {
 
 hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t s) {
   if (a.groups) {
-    if (a.tile_rows == 16) launch_attention_narrow<1>(a, s);
-    else if (a.tile_rows == 32) launch_attention_narrow<2>(a, s);
+    if (a.tile_rows == 16) launch_attention_narrow<1>(a, a.groups, s);
+    else if (a.tile_rows == 32) launch_attention_narrow<2>(a, a.groups, s);
     else launch_attention<0, true>(a, a.groups, s);
     a.type == kBf16 ? launch_join<kBf16>(a, s) : launch_join<kF16>(a, s);
     return hipGetLastError();
   }
-  const int tokens = kAttnRows / (int)a.group.d;
+  const int tokens = a.tile_rows / (int)a.group.d;
   const int64_t tiles = (a.T / tokens + (a.S < a.T ? a.S : a.T)) * a.kv_heads;   // as many as there can be
   constexpr int64_t kPiece = int64_t(1) << 23;                     // (a launch holds fewer than 2^32 threads)
   CacheArgs piece = a;
-  for (piece.t0 = 0; piece.t0 < tiles; piece.t0 += kPiece) launch_attention<0, false>(piece, (uint32_t)(tiles - piece.t0 < kPiece ? tiles - piece.t0 : kPiece), s);
+  for (piece.t0 = 0; piece.t0 < tiles; piece.t0 += kPiece) {
+    const uint32_t n = (uint32_t)(tiles - piece.t0 < kPiece ? tiles - piece.t0 : kPiece);
+    if (a.tile_rows == 16) launch_attention_narrow<1>(piece, n, s);
+    else if (a.tile_rows == 32) launch_attention_narrow<2>(piece, n, s);
+    else launch_attention<0, false>(piece, n, s);
+  }
   return hipGetLastError();
 }
 

@@ -4,8 +4,9 @@
 namespace axe {
 
 template <>
-void launch_attention_narrow<2>(const CacheArgs& a, hipStream_t s) {
-  launch_attention<2, true>(a, a.groups, s);
+void launch_attention_narrow<2>(const CacheArgs& a, uint32_t groups, hipStream_t s) {
+  if (a.groups) launch_attention<2, true>(a, groups, s);
+  else launch_attention<2, false>(a, groups, s);
 }
 
 }  // namespace axe
