@@ -210,7 +210,7 @@ int axe_cache_append(const axe_cache_desc_t* g, const void* d_q, const void* d_k
 int64_t axe_cache_attention_workspace(const axe_cache_desc_t* g) {
   return guarded("axe_cache_attention_workspace", [&]() -> int64_t {
     if (int rc = check_cache(g, "axe_cache_attention_workspace")) return rc;
-    return attn_workspace_words(attn_shape(g->T, g->S, g->kv_heads, g->q_heads / g->kv_heads, g->head_dim, (int64_t)g->max_pages * g->page_tokens), g->head_dim);
+    return attn_workspace_words(attn_shape(g->T, g->S, g->kv_heads, g->q_heads / g->kv_heads, g->head_dim, (int64_t)g->max_pages * g->page_tokens, g->causal ? g->window : 0), g->head_dim);
   });
 }
 
@@ -229,7 +229,7 @@ int axe_cache_attention(const axe_cache_desc_t* g, const void* d_q, const void* 
     if (int rc = kept_cache_plan(g, fn, {true, false, true}, kept)) return rc;
     const CachePlan& p = *kept;
     const int G = g->q_heads / g->kv_heads, eb = 2, cb = fp8 ? 1 : 2;
-    const AttnShape shape = attn_shape(g->T, g->S, g->kv_heads, G, g->head_dim, (int64_t)g->max_pages * g->page_tokens);
+    const AttnShape shape = attn_shape(g->T, g->S, g->kv_heads, G, g->head_dim, (int64_t)g->max_pages * g->page_tokens, g->causal ? g->window : 0);
     const int64_t words = attn_workspace_words(shape, g->head_dim);
     if (words > 0 && (!d_ws || ws_elems < words)) return invalid(fn, "the workspace is smaller than axe_cache_attention_workspace");
     const Tables t = tables(g, d_seq_rows, d_lengths, d_page_table);

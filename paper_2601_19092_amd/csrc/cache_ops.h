@@ -69,20 +69,25 @@ inline int attn_columns(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 // Workgroups that the chip holds at once.
 inline int attn_slots(int D) { return attn_columns(D) <= 128 ? 512 : 256; }
 
-// groups: workgroups of the split form, 0: every tile a workgroup's.  The keys of a tile are split among workgroups unless there are tiles enough to fill the chip some times over, or so few
-// keys (of narrow tiles) that the second launch takes longer.
+// groups: workgroups of the split form, 0: every tile a workgroup's.  Splitting a tile's keys among workgroups costs partial results and a second launch, some 20 us of wide tiles, for which ten blocks
+// of keys are done.  It is not done where there are tiles enough to fill the chip some times over, nor where all workgroups are through with their tiles by the time: 24 blocks at most, and 16
+// on average that a place on the chip is idle.  us, split / whole: 512 new tokens, 32 heads over 4, 39 / 18; 1024, 32 over 8, 51 / 29; 24 x 100 over 1100 keys, 16 heads of 64 columns, 56 / 32;
+// 256 over 2048 keys 42 / 75.  Narrow tiles take a microsecond for 64 keys: one token over 500 keys 13 / 14, over 32 12.8 / 6.7.
 // Rows of a tile: as many as the sequences have on average, up to 32; from there on 128.
 struct AttnShape {
   int tile_rows, groups, ws_rows;
 };
-inline AttnShape attn_shape(int64_t T, int S, int kv_heads, int group, int D, int64_t capacity) {
+// window: keys that a token sees at most, 0: all.
+inline AttnShape attn_shape(int64_t T, int S, int kv_heads, int group, int D, int64_t capacity, int window) {
   AttnShape r = {kAttnRows, 0, 0};
   if (T == 0 || S == 0) return r;
   const int64_t wide = kAttnRows / group, tiles = (T + wide - 1) / wide * kv_heads;
   if (S > kAttnSplitSeqs || tiles >= 2 * (int64_t)attn_slots(D)) return r;
   const int64_t rows = (T + S - 1) / S * group;
   if (rows <= 32) r.tile_rows = rows <= 16 ? 16 : 32;
-  if (r.tile_rows <= 32 && capacity <= kAttnFewKeys) return r;
+  const int64_t reach = window && window + wide < capacity ? window + wide : capacity, blocks = (reach + kAttnKeys - 1) / kAttnKeys, slots = attn_slots(D);
+  const int64_t idle = (slots - tiles % slots) % slots;
+  if (r.tile_rows <= 32 ? reach <= kAttnFewKeys : blocks <= 24 && blocks * idle <= 16 * slots) return r;
   r.groups = attn_slots(D);
   const int64_t tokens = r.tile_rows / group, most = T < tokens ? T * group : r.tile_rows;
   r.ws_rows = (int)((most + 15) / 16 * 16);
