@@ -151,8 +151,10 @@ def test_attention_buffers():
         assert attention_rc(scale=scale) == B.AXE_EINVAL, scale
     assert attention_rc(window=-1) == B.AXE_EINVAL and attention_rc(window=4, causal=False) == B.AXE_EUNSUPPORTED
     assert attention_rc(out=P[0]) == B.AXE_EINVAL and attention_rc(out=P[8] + 64) == B.AXE_EINVAL and attention_rc(out=P[6]) == B.AXE_EINVAL
-    assert host().axe_cache_attention_workspace(desc().ref) > 0
-    assert attention_rc(n=0) == B.AXE_EINVAL and attention_rc(ws=None) == B.AXE_EINVAL and attention_rc(ws=P[7]) == B.AXE_EINVAL and attention_rc(ws=P[12] + 4) == B.AXE_EINVAL
+    assert host().axe_cache_attention_workspace(desc().ref) == 0 and attention_rc(ws=None) == B.AXE_EHIP   # (few keys: no parts)
+    assert host().axe_cache_attention_workspace(desc(most=300).ref) > 0
+    for kw in (dict(n=0), dict(ws=None), dict(ws=P[7]), dict(ws=P[12] + 4)):
+        assert attention_rc(most=300, **kw) == B.AXE_EINVAL, kw
     assert host().axe_cache_attention_workspace(desc(T=0).ref) == 0 and host().axe_cache_attention_workspace(desc(D=60).ref) == B.AXE_EUNSUPPORTED
     assert host().axe_cache_attention_workspace(None) == B.AXE_EINVAL
     assert host().axe_cache_attention(None, *[None] * 10, 0, None) == B.AXE_EINVAL and host().axe_cache_append(None, *[None] * 13) == B.AXE_EINVAL
@@ -177,3 +179,18 @@ def test_refusals_under_address_and_undefined_behaviour_sanitizers():
                        cwd=S.ROOT, env=env, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=900)
     assert "AddressSanitizer" not in p.stdout and "runtime error:" not in p.stdout, p.stdout[-4000:]
     assert p.returncode == 0 and " passed" in p.stdout, p.stdout[-4000:]
+
+
+def test_workspaces_follow_from_sizes():
+    """Words for the partial results of all workgroups: none where every tile is a workgroup's; the same for the same sizes; enough for the rows of a tile."""
+    words = lambda **kw: host().axe_cache_attention_workspace(desc(**kw).ref)  # noqa: E731
+    part = lambda rows, cols: 2 * (512 if cols <= 128 else 256) * (4 + 2 * rows + rows * cols)  # noqa: E731
+    assert words(T=2, S=2, most=300) == part(16, 64) and words(T=1, S=1, Hq=32, Hkv=4, D=128, most=100) == part(16, 128)
+    assert words(T=2, S=2, Hq=32, Hkv=1, most=300) == part(32, 64)     # 32 rows for a token
+    assert words(T=80, S=2, most=300) == part(128, 64) and words(T=40, S=1, Hq=4, Hkv=4, D=256, most=300) == part(48, 256)
+    assert words(T=1 << 20, S=2, most=300) == 0                        # tiles enough
+    assert words(T=5000, S=5000, most=300) == 0                        # more sequences than are cut
+    assert words(T=2, S=2, most=16) == 0 and words(T=2, S=2, most=17) > 0   # 256 keys, 272
+    for kw in (dict(T=2, S=2, most=300), dict(T=600, S=3, Hq=8, Hkv=2, most=200)):
+        assert words(**kw) == words(**kw, window=100000) and words(**kw) > 0
+        assert words(cache=B.AXE_FP8_E4M3, **kw) == words(**kw)
