@@ -408,22 +408,35 @@ struct Attention {
       bring<2>(false, f, 0, lds_at(&sh.kv[stage][0][wave * 16 * ROW]));
       bring<2>(true, f, 0, lds_at(&sh.kv[stage][1][wave * 16 * ROW]));
     } else {
-      int page, slot;
+      const uint8_t *kb = (const uint8_t*)a.k_cache + it.head * a.kp.head, *vb = (const uint8_t*)a.v_cache + it.head * a.vp.head;
+      int64_t at = 0;                                              // of the scales: lane i brings those of key i
+      bool on = true;
+      if (f.side_by_side) {
+        kb += f.page * a.kp.page + f.slot * a.kp.slot, vb += f.page * a.vp.page + f.slot * a.vp.slot;
 #pragma unroll
-      for (int i = 0; i < S2::NI; ++i) {
-        const int row = i * S2::RPI + lane / S2::CH, kc = (lane % S2::CH ^ S2::place(false, row)) * 8, vc = (lane % S2::CH ^ S2::place(true, row)) * 8;
-        const bool on = where(first + row, page, slot);
-        const int64_t kat = page * a.kp.page + slot * a.kp.slot + it.head * a.kp.head, vat = page * a.vp.page + slot * a.vp.slot + it.head * a.vp.head;
-        kreg[i] = vreg[i] = u32x2{};
-        if (on && kc < a.D) kreg[i] = *(const u32x2*)((const uint8_t*)a.k_cache + kat + kc);
-        if (on && vc < a.D) vreg[i] = *(const u32x2*)((const uint8_t*)a.v_cache + vat + vc);
+        for (int i = 0; i < S2::NI; ++i) {
+          const int row = i * S2::RPI + lane / S2::CH, kc = (lane % S2::CH ^ S2::k(row)) * 8, vc = (lane % S2::CH ^ S2::v(row)) * 8;
+          kreg[i] = vreg[i] = u32x2{};
+          if (kc < a.D) kreg[i] = *(const u32x2*)(kb + (uint32_t)(row * (int)a.kp.slot + kc));
+          if (vc < a.D) vreg[i] = *(const u32x2*)(vb + (uint32_t)(row * (int)a.vp.slot + vc));
+        }
+        at = (int64_t)f.page * a.page.d + f.slot + (lane & 15);
+      } else {
+        int ln = lane, page, slot;
+        asm volatile("" : "+v"(ln));
+#pragma unroll
+        for (int i = 0; i < S2::NI; ++i) {
+          const int row = i * S2::RPI + ln / S2::CH, kc = (ln % S2::CH ^ S2::k(row)) * 8, vc = (ln % S2::CH ^ S2::v(row)) * 8;
+          const bool is = where(first + row, page, slot);
+          kreg[i] = vreg[i] = u32x2{};
+          if (is && kc < a.D) kreg[i] = *(const u32x2*)(kb + page * a.kp.page + slot * a.kp.slot + kc);
+          if (is && vc < a.D) vreg[i] = *(const u32x2*)(vb + page * a.vp.page + slot * a.vp.slot + vc);
+        }
+        on = where(first + (ln & 15), page, slot);
+        at = (int64_t)page * a.page.d + slot;
       }
-      const bool on = where(first + (lane & 15), page, slot);      // lane i brings the scales of key i
       sreg[0] = sreg[1] = 0;
-      if (on) {
-        const int64_t at = ((int64_t)page * a.page.d + slot) * a.kv_heads + it.head;
-        sreg[0] = a.k_scales[at], sreg[1] = a.v_scales[at];
-      }
+      if (on) sreg[0] = a.k_scales[at * a.kv_heads + it.head], sreg[1] = a.v_scales[at * a.kv_heads + it.head];
     }
     if (lane == 0) sh.there[stage][wave] = (uint16_t)there;
   }
@@ -553,7 +566,7 @@ struct Attention {
         const float* sc = &sh.scales[stage][1][k * 16 + (e >> 1) * 8 + h * 4 + (e & 1) * 2];
         const float v0 = sc[0] * by_v, v1 = sc[1] * by_v, t0 = x * v0, t1 = y * v1;
         p[k][e] = pack2<TYPE>(t0, t1);
-        l += weight(x, t0, v0, half<TYPE>(p[k][e], 0)) + weight(y, t1, v1, half<TYPE>(p[k][e], 1));
+        l += x + y;                                                // (not as they are rounded, as in run_narrow: here the vector unit is what bounds)
       } else {
         p[k][e] = pack2<TYPE>(x, y);
         l = add2<TYPE>(p[k][e], l);
