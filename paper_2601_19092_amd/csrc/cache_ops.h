@@ -63,7 +63,7 @@ constexpr int kAttnRows = 128;     // rows (tokens x query heads of one head of 
 constexpr int kAttnKeys = 64;      // keys of a block
 constexpr int kAttnMaxGroup = 128; // query heads of a head of the cache
 constexpr int kAttnSplitSeqs = 4096;
-constexpr int kAttnFewKeys = 256;
+constexpr int kAttnFewKeys = 768;
 
 inline int attn_columns(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 // Workgroups that the chip holds at once.
@@ -72,7 +72,8 @@ inline int attn_slots(int D) { return attn_columns(D) <= 128 ? 512 : 256; }
 // groups: workgroups of the split form, 0: every tile a workgroup's.  Splitting a tile's keys among workgroups costs partial results and a second launch, some 20 us of wide tiles, for which ten blocks
 // of keys are done.  It is not done where there are tiles enough to fill the chip some times over, nor where all workgroups are through with their tiles by the time: 24 blocks at most, and 16
 // on average that a place on the chip is idle.  us, split / whole: 512 new tokens, 32 heads over 4, 39 / 18; 1024, 32 over 8, 51 / 29; 24 x 100 over 1100 keys, 16 heads of 64 columns, 56 / 32;
-// 256 over 2048 keys 42 / 75.  Narrow tiles take a microsecond for 64 keys: one token over 500 keys 13 / 14, over 32 12.8 / 6.7.
+// 256 over 2048 keys 42 / 75.  Narrow tiles, by the same: up to 768 keys, twice that where 64 tiles or more share the chip's bandwidth; one token, 32 heads over 4, of 512 keys 12.4 / 11.0, of 1024
+// 14.4 / 16.3; 16 tokens, 32 over 8, of 1536 27.3 / 25.2; 64 tokens of 1024 51.8 / 46.5.
 // Rows of a tile: as many as the sequences have on average, up to 32; from there on 128.
 struct AttnShape {
   int tile_rows, groups, ws_rows;
@@ -87,7 +88,8 @@ inline AttnShape attn_shape(int64_t T, int S, int kv_heads, int group, int D, in
   if (rows <= 32) r.tile_rows = rows <= 16 ? 16 : 32;
   const int64_t reach = window && window + wide < capacity ? window + wide : capacity, blocks = (reach + kAttnKeys - 1) / kAttnKeys, slots = attn_slots(D);
   const int64_t idle = (slots - tiles % slots) % slots;
-  if (r.tile_rows <= 32 ? reach <= kAttnFewKeys : blocks <= 24 && blocks * idle <= 16 * slots) return r;
+  const int64_t narrow = r.tile_rows <= 32 ? r.tile_rows / group : 1, narrows = (T + narrow - 1) / narrow * kv_heads;
+  if (r.tile_rows <= 32 ? reach <= (narrows < 64 ? kAttnFewKeys : 2 * kAttnFewKeys) : blocks <= 24 && blocks * idle <= 16 * slots) return r;
   r.groups = attn_slots(D);
   const int64_t tokens = r.tile_rows / group, most = T < tokens ? T * group : r.tile_rows;
   r.ws_rows = (int)((most + 15) / 16 * 16);
