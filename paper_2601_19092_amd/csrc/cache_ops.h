@@ -88,7 +88,7 @@ inline AttnShape attn_shape(int64_t T, int S, int kv_heads, int group, int D, in
   if (rows <= 32) r.tile_rows = rows <= 16 ? 16 : 32;
   const int64_t reach = window && window + wide < capacity ? window + wide : capacity, blocks = (reach + kAttnKeys - 1) / kAttnKeys, slots = attn_slots(D);
   const int64_t idle = (slots - tiles % slots) % slots;
-  const int64_t narrow = r.tile_rows <= 32 ? r.tile_rows / group : 1, narrows = (T + narrow - 1) / narrow * kv_heads;
+  const int64_t narrows = (T < S ? T : S) * kv_heads;              // narrow tiles, of sequences that all have new tokens
   if (r.tile_rows <= 32 ? reach <= (narrows < 64 ? kAttnFewKeys : 2 * kAttnFewKeys) : blocks <= 24 && blocks * idle <= 16 * slots) return r;
   r.groups = attn_slots(D);
   const int64_t tokens = r.tile_rows / group, most = T < tokens ? T * group : r.tile_rows;

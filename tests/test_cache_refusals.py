@@ -191,7 +191,7 @@ def test_workspaces_follow_from_sizes():
     assert words(T=1 << 20, S=2, most=300) == 0                        # tiles enough
     assert words(T=5000, S=5000, most=300) == 0                        # more sequences than are cut
     assert words(T=2, S=2, most=48) == 0 and words(T=2, S=2, most=49) > 0   # 768 keys, 784
-    assert words(T=32, S=32, most=96) == 0 and words(T=32, S=32, most=97) > 0
+    assert words(T=32, S=32, most=96) == 0 and words(T=32, S=32, most=97) > 0 and words(T=31, S=31, most=96) > 0
     for kw in (dict(T=2, S=2, most=300), dict(T=600, S=3, Hq=8, Hkv=2, most=200)):
         assert words(**kw) == words(**kw, window=100000) and words(**kw) > 0
         assert words(cache=B.AXE_FP8_E4M3, **kw) == words(**kw)
