@@ -74,7 +74,8 @@ inline int attn_slots(int D) { return attn_columns(D) <= 128 ? 512 : 256; }
 // on average that a place on the chip is idle.  us, split / whole: 512 new tokens, 32 heads over 4, 39 / 18; 1024, 32 over 8, 51 / 29; 24 x 100 over 1100 keys, 16 heads of 64 columns, 56 / 32;
 // 256 over 2048 keys 42 / 75.  Narrow tiles, by the same: up to 768 keys, twice that where 64 tiles or more share the chip's bandwidth; one token, 32 heads over 4, of 512 keys 12.4 / 11.0, of 1024
 // 14.4 / 16.3; 16 tokens, 32 over 8, of 1536 27.3 / 25.2; 64 tokens of 1024 51.8 / 46.5.
-// Rows of a tile: as many as the sequences have on average, up to 32; from there on 128.
+// Rows of a tile: as many as the sequences have on average, up to 32; from there on 128, or 32 where 128 would leave most of the chip without a tile.  us, 128 / 32 rows: 38 wide tiles, 600 new
+// tokens over 700 keys of 256 columns, 39 / 30; 32, 128 tokens over 8192, 77 / 69; 16, 64 over 2048, 36 / 34; 64, 256 over 2048, 42 / 49; 128, 100 of each of 8 over 2200, 54 / 79.
 struct AttnShape {
   int tile_rows, groups, ws_rows;
 };
@@ -85,13 +86,14 @@ inline AttnShape attn_shape(int64_t T, int S, int kv_heads, int group, int D, in
   const int64_t wide = kAttnRows / group, tiles = (T + wide - 1) / wide * kv_heads;
   if (S > kAttnSplitSeqs || tiles >= 2 * (int64_t)attn_slots(D)) return r;
   const int64_t rows = (T + S - 1) / S * group;
-  if (rows <= 32) r.tile_rows = rows <= 16 ? 16 : 32;
+  const int64_t whole = T < S ? T : S, wides = (T + wide - 1) / wide > whole ? tiles : whole * kv_heads;   // (as all sequences have new tokens)
+  if (rows <= 32 || (group <= 32 && wides < 48)) r.tile_rows = rows <= 16 ? 16 : 32;
   const int64_t reach = window && window + wide < capacity ? window + wide : capacity, blocks = (reach + kAttnKeys - 1) / kAttnKeys, slots = attn_slots(D);
   const int64_t idle = (slots - tiles % slots) % slots;
-  const int64_t narrows = (T < S ? T : S) * kv_heads;              // narrow tiles, of sequences that all have new tokens
+  const int64_t tokens = r.tile_rows / group, cut = (T + tokens - 1) / tokens, narrows = (cut > whole ? cut : whole) * kv_heads;
   if (r.tile_rows <= 32 ? reach <= (narrows < 64 ? kAttnFewKeys : 2 * kAttnFewKeys) : blocks <= 24 && blocks * idle <= 16 * slots) return r;
   r.groups = attn_slots(D);
-  const int64_t tokens = r.tile_rows / group, most = T < tokens ? T * group : r.tile_rows;
+  const int64_t most = T < tokens ? T * group : r.tile_rows;
   r.ws_rows = (int)((most + 15) / 16 * 16);
   return r;
 }

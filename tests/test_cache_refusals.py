@@ -187,11 +187,13 @@ def test_workspaces_follow_from_sizes():
     part = lambda rows, cols: 2 * (512 if cols <= 128 else 256) * (4 + 2 * rows + rows * cols)  # noqa: E731
     assert words(T=2, S=2, most=300) == part(16, 64) and words(T=1, S=1, Hq=32, Hkv=4, D=128, most=100) == part(16, 128)
     assert words(T=2, S=2, Hq=32, Hkv=1, most=300) == part(32, 64)     # 32 rows for a token
-    assert words(T=80, S=2, most=300) == part(128, 64) and words(T=40, S=1, Hq=4, Hkv=4, D=256, most=300) == part(48, 256)
+    assert words(T=80, S=2, most=300) == part(32, 64) and words(T=1600, S=2, most=300) == part(128, 64)      # 4 wide tiles, 50
+    assert words(T=100, S=1, Hq=64, Hkv=1, D=256, most=300) == part(128, 256) and words(T=20, S=1, Hq=48, Hkv=48, D=256, most=300) == part(32, 256)
+    assert words(T=40, S=1, Hq=48, Hkv=48, D=256, most=300) == part(48, 256)
     assert words(T=1 << 20, S=2, most=300) == 0                        # tiles enough
     assert words(T=5000, S=5000, most=300) == 0                        # more sequences than are cut
     assert words(T=2, S=2, most=48) == 0 and words(T=2, S=2, most=49) > 0   # 768 keys, 784
     assert words(T=32, S=32, most=96) == 0 and words(T=32, S=32, most=97) > 0 and words(T=31, S=31, most=96) > 0
-    for kw in (dict(T=2, S=2, most=300), dict(T=600, S=3, Hq=8, Hkv=2, most=200)):
+    for kw in (dict(T=2, S=2, most=300), dict(T=600, S=3, Hq=8, Hkv=2, most=200), dict(T=2400, S=3, Hq=8, Hkv=2, most=200)):
         assert words(**kw) == words(**kw, window=100000) and words(**kw) > 0
         assert words(cache=B.AXE_FP8_E4M3, **kw) == words(**kw)

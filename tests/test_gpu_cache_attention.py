@@ -5,7 +5,7 @@ Tolerances.  U = 2^-24, H = half a step of the 16-bit type relative to the value
   the weights' rounding for the product with V             H A
   the scores: D products summed in fp32, the scaling, the exponential: each weight is off by a factor of at most e^(2 E), E = (D + 8) U reach + 4 U, reach = scale max_j sum_d |q_d k_jd|
   the sums over n keys, numerator and denominator          2 (n + 64) U A
-  fp16's smallest steps: a term is held as w 2^15 (e4m3 caches: w 2^8 times a scale that is at most 1 of the largest's power of two): n 2^-32 max |v|
+  fp16's smallest steps: a term is held as at least w 2^9, w relative to the largest (e4m3 caches: times a scale that is more than half a power of two), so off by 2^-34 (2^-33): n 2^-32 max |v|
 """
 import numpy as np
 import pytest
@@ -21,6 +21,9 @@ U = 2.0 ** -24
 CODE = {"bf16": B.AXE_BF16, "f16": B.AXE_F16, "fp8": B.AXE_FP8_E4M3}
 TORCH = {"bf16": torch.bfloat16, "f16": torch.float16, "fp8": torch.float8_e4m3fn}
 HALF = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+WIDE = (66, 2)                                                         # 33 query heads to a head of the cache: tiles of 128 rows, whatever the batch; three tokens each
 
 
 def f64(t):
@@ -103,13 +106,13 @@ class Batch:
 
 @pytest.mark.parametrize("dtype, cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "fp8"), ("f16", "fp8")])
 @pytest.mark.parametrize("D", [64, 128, 256, 16, 80, 8, 136])
-@pytest.mark.parametrize("new", [[3, 1, 70], [1, 1, 1], [9, 8, 7]])    # tiles of 128, 16 and 32 rows
-def test_types_and_columns(dtype, cache, D, new):
+@pytest.mark.parametrize("new, heads", [([1, 1, 1], (4, 2)), ([9, 8, 7], (4, 2)), ([3, 1, 70], (4, 2)), ([1, 2, 9], WIDE), ([3, 1, 20], (48, 48))])   # tiles of 16, 32, 32, 128 and 128 rows
+def test_types_and_columns(dtype, cache, D, new, heads):
     if cache == "fp8" and D % 16:
         with pytest.raises(B.AxeError, match="head_dim"):
-            Batch([130, 8, 77], new, 4, 2, D, 16, dtype, cache, seed=D).run()
+            Batch([130, 9, 77], new, *heads, D, 16, dtype, cache, seed=D).run()
         return
-    b = Batch([530, 8, 77], new, 4, 2, D, 16, dtype, cache, seed=D)
+    b = Batch([530, 9, 77], new, *heads, D, 16, dtype, cache, seed=D)
     b.check(b.run())
 
 
@@ -120,16 +123,16 @@ def test_heads(Hq, Hkv):
 
 
 @pytest.mark.parametrize("page", [1, 3, 16, 24, 64, 100, 1000])
-@pytest.mark.parametrize("new", [1, 50])
-def test_pages(page, new):
-    b = Batch([200, 63, 64, 65], [new] * 4, 4, 2, 128, page, seed=page)
+@pytest.mark.parametrize("new, heads", [(1, (4, 2)), (50, (4, 2)), (5, WIDE)])
+def test_pages(page, new, heads):
+    b = Batch([200, 63, 64, 65], [new] * 4, *heads, 128, page, seed=page)
     b.check(b.run())
 
 
 @pytest.mark.parametrize("causal, window", [(False, 0), (True, 1), (True, 5), (True, 64), (True, 70), (True, 1000)])
-@pytest.mark.parametrize("lengths, new", [([300], [1]), ([300, 20, 150], [150, 20, 3])])
-def test_masks(causal, window, lengths, new):
-    b = Batch(lengths, new, 4, 2, 64, 16, seed=window)
+@pytest.mark.parametrize("lengths, new, heads", [([300], [1], (4, 2)), ([300, 20, 150], [150, 20, 3], (4, 2)), ([300, 20, 150], [20, 7, 1], WIDE), ([300, 20, 150], [15, 20, 1], (48, 48))])
+def test_masks(causal, window, lengths, new, heads):
+    b = Batch(lengths, new, *heads, 64, 16, seed=window)
     b.check(b.run(causal=causal, window=window), causal, window)
 
 
@@ -139,8 +142,9 @@ def test_masks(causal, window, lengths, new):
 def test_layouts_of_the_cache(order, gap, page, cache):
     if cache == "fp8":
         gap = gap // 16 * 16
-    b = Batch([150, 40], [1, 1] if gap else [20, 30], 4, 2, 128, page, "bf16", cache, seed=gap, order=order, gap=gap)
-    b.check(b.run())
+    for new, heads in (([1, 1] if gap else [20, 30], (4, 2)), ([4, 3], WIDE)):
+        b = Batch([150, 40], new, *heads, 128, page, "bf16", cache, seed=gap, order=order, gap=gap)
+        b.check(b.run())
 
 
 @pytest.mark.parametrize("new", [[1, 1], [30, 40]])
@@ -161,11 +165,12 @@ def test_layouts_of_rows(new):
     assert torch.equal(out, before), "what lies between the rows is left as it was"
 
 
+@pytest.mark.parametrize("heads", [(4, 2), WIDE])
 @pytest.mark.parametrize("new", [[0, 3, 0, 1, 5, 0], [0, 40, 0, 30, 5, 0], [0, 0, 0, 0, 0, 0]])
-def test_sequences_without_new_tokens_without_keys_and_rows_of_none(new):
-    b = Batch([70, 80, 0, 90, 33, 1], new, 4, 2, 64, 16, seed=5)
+def test_sequences_without_new_tokens_without_keys_and_rows_of_none(new, heads):
+    b = Batch([70, 80, 0, 90, 33, 1], new, *heads, 64, 16, seed=5)
     if b.T == 0:                                                       # rows, but none of a sequence's
-        b.T, b.q = 3, torch.randn(3, 4, 64).to(torch.bfloat16)
+        b.T, b.q = 3, torch.randn(3, heads[0], 64).to(torch.bfloat16)
     lengths = [70, 80, 0, 0, 2, 1]                                     # more new tokens than tokens: the first are at negative positions and see nothing
     b.check(b.run(lengths=torch.tensor(lengths, dtype=torch.int32)), lengths=lengths)
     b.check(b.run(lengths=torch.tensor(lengths, dtype=torch.int32), causal=False), causal=False, lengths=lengths)
@@ -176,10 +181,10 @@ def test_sequences_without_new_tokens_without_keys_and_rows_of_none(new):
 
 
 @pytest.mark.parametrize("page", [16, 7])
-@pytest.mark.parametrize("new", [[1, 1], [50, 60]])
+@pytest.mark.parametrize("new, heads", [([1, 1], (4, 2)), ([50, 60], (4, 2)), ([4, 5], WIDE)])
 @pytest.mark.parametrize("cache", ["bf16", "fp8"])
-def test_pages_that_are_none_and_lengths_past_the_table(page, new, cache):
-    b = Batch([200, 150], new, 4, 2, 64, page, "bf16", cache, seed=7)
+def test_pages_that_are_none_and_lengths_past_the_table(page, new, heads, cache):
+    b = Batch([200, 150], new, *heads, 64, page, "bf16", cache, seed=7)
     table = b.table.clone()
     table[0, 1], table[0, 3], table[1, 0] = -1, b.pages, 2 ** 31 - 1
     table[1, 2:4] = -(2 ** 31)
@@ -192,17 +197,18 @@ def test_pages_that_are_none_and_lengths_past_the_table(page, new, cache):
 
 
 @pytest.mark.parametrize("garbage", [float("nan"), float("inf")])
-@pytest.mark.parametrize("new", [[1, 1], [9, 9], [60, 64]])
+@pytest.mark.parametrize("new, heads", [([1, 1], (4, 2)), ([9, 9], (4, 2)), ([60, 64], (4, 2)), ([4, 3], WIDE), ([10, 20], (48, 48))])
 @pytest.mark.parametrize("dtype, cache, D, page", [("bf16", "bf16", 128, 16), ("f16", "f16", 80, 16), ("bf16", "bf16", 64, 10), ("bf16", "fp8", 128, 16)])
-def test_what_no_sequence_holds_has_no_part(garbage, new, dtype, cache, D, page):
+def test_what_no_sequence_holds_has_no_part(garbage, new, heads, dtype, cache, D, page):
     if cache == "fp8" and garbage == float("inf"):
         garbage = float("nan")                                         # (e4m3 has no infinities)
-    b = Batch([100, 65], new, 4, 2, D, page, dtype, cache, seed=9, garbage=garbage)
+    b = Batch([100, 65], new, *heads, D, page, dtype, cache, seed=9, garbage=garbage)
     b.check(b.run())
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
-@pytest.mark.parametrize("length, new, Hq, Hkv, D, window", [(90, 40, 4, 1, 128, 0), (90, 8, 2, 1, 64, 0), (300, 200, 1, 1, 64, 0), (700, 130, 8, 2, 256, 0), (90, 40, 4, 1, 128, 20), (100, 12, 2, 1, 128, 30)])
+@pytest.mark.parametrize("length, new, Hq, Hkv, D, window", [(90, 40, 4, 1, 128, 0), (90, 8, 2, 1, 64, 0), (300, 200, 1, 1, 64, 0), (700, 130, 8, 2, 256, 0), (90, 40, 4, 1, 128, 20), (100, 12, 2, 1, 128, 30),
+                                                                (90, 9, *WIDE, 128, 0), (90, 9, *WIDE, 64, 12), (300, 140, 48, 48, 64, 0), (700, 9, *WIDE, 256, 0), (2000, 9, *WIDE, 128, 0)])
 def test_values_that_are_not_finite_reach_those_that_see_them_alone(bad, length, new, Hq, Hkv, D, window):
     """A value that is not finite at one new token's place (and, with a window, at an old one): the tokens before it (behind the window) come out as if it were not there, the others not finite."""
     b = Batch([length], [new], Hq, Hkv, D, 16, seed=11)
@@ -240,17 +246,17 @@ def test_keys_that_are_not_finite_where_masked():
 
 @pytest.mark.parametrize("std, scale", [(30.0, None), (1e-3, None), (1.0, 1e-6), (4.0, 3.0), (1.0, 2.0 ** -100)])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("new", [1, 40])
-def test_sizes_of_scores(std, scale, dtype, new):
-    b = Batch([500], [new], 4, 2, 64, 16, dtype, seed=15, std=std)
+@pytest.mark.parametrize("new, heads", [(1, (4, 2)), (40, (4, 2)), (5, WIDE)])
+def test_sizes_of_scores(std, scale, dtype, new, heads):
+    b = Batch([500], [new], *heads, 64, 16, dtype, seed=15, std=std)
     b.check(b.run(scale=scale), scale=scale)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("new", [1, 40])
-def test_scales_of_an_e4m3_cache_far_apart(dtype, new):
+@pytest.mark.parametrize("new, heads", [(1, (4, 2)), (40, (4, 2)), (5, WIDE)])
+def test_scales_of_an_e4m3_cache_far_apart(dtype, new, heads):
     """Zeros, tiny and large ones side by side: terms times scales stay inside fp16's range."""
-    b = Batch([300], [new], 4, 2, 64, 16, dtype, "fp8", seed=17)
+    b = Batch([300], [new], *heads, 64, 16, dtype, "fp8", seed=17)
     g = torch.Generator().manual_seed(2)
     sc = 2.0 ** torch.randint(-12, 8 if dtype == "f16" else 14, b.scales[1].shape, generator=g).float()
     sc[torch.rand(sc.shape, generator=g) < 0.2] = 0.0
@@ -294,7 +300,8 @@ def dense(b, lengths, new, D, causal=True, window=0):
     ([20000], [1], 8, 1, 128, 64, "bf16", "bf16", 0), ([9000, 3, 700], [1, 1, 1], 4, 4, 64, 16, "f16", "f16", 0), ([30000], [1], 4, 2, 64, 16, "bf16", "fp8", 0), ([5000, 900], [3, 1], 8, 1, 128, 24, "bf16", "bf16", 0),
     ([2500], [700], 4, 1, 128, 16, "bf16", "bf16", 0), ([3000, 40, 1800], [260, 40, 1], 8, 2, 64, 7, "f16", "f16", 0), ([2000, 1500], [500, 900], 2, 2, 256, 32, "bf16", "bf16", 0),
     ([4000], [400], 4, 1, 128, 16, "bf16", "fp8", 0), ([6000, 5000], [300, 1], 4, 1, 64, 16, "f16", "fp8", 1100), ([1200] * 3, [1200, 600, 1], 16, 16, 64, 16, "bf16", "bf16", 0),
-    ([5000], [5000], 2, 2, 64, 64, "f16", "f16", 0), ([150] * 70, [2] * 70, 16, 16, 64, 16, "bf16", "bf16", 0), ([700] * 80, [1] * 80, 2, 1, 64, 16, "bf16", "bf16", 0), ([600] * 70, [9] * 70, 4, 1, 64, 16, "bf16", "bf16", 0)])
+    ([5000], [5000], 2, 2, 64, 64, "f16", "f16", 0), ([150] * 70, [2] * 70, 16, 16, 64, 16, "bf16", "bf16", 0), ([700] * 80, [1] * 80, 2, 1, 64, 16, "bf16", "bf16", 0), ([600] * 70, [9] * 70, 4, 1, 64, 16, "bf16", "bf16", 0),
+    ([3000, 700], [9, 200], *WIDE, 128, 16, "bf16", "bf16", 0), ([3000, 40], [60, 1], 48, 48, 64, 24, "f16", "fp8", 0), ([2000, 900], [40, 3], *WIDE, 256, 16, "bf16", "fp8", 0), ([1700] * 70, [2] * 70, 33, 1, 64, 16, "bf16", "bf16", 0)])
 def test_long_and_many(lengths, new, Hq, Hkv, D, page, dtype, cache, window):
     """Keys split among workgroups and not, cuts inside tiles, batches above 64 sequences; and the same bits a second time."""
     b = Batch(lengths, new, Hq, Hkv, D, page, dtype, cache, seed=19)
@@ -316,9 +323,9 @@ def test_more_sequences_than_a_workgroup_surveys():
 
 def test_a_cache_past_2_to_the_31_bytes():
     """Pages far apart: places whose offsets 32 bits do not hold, in pages of 16 tokens and of 24."""
-    for page, new in ((16, 1), (24, 1), (16, 40), (24, 40)):
+    for page, new, heads in ((16, 1, 4), (24, 1, 4), (16, 20, 4), (24, 20, 4), (16, 20, 33), (24, 20, 33)):
         Hkv, D, far = 1, 64, 3 * 2 ** 30 // 2                           # elements between pages: 3 GiB
-        small = Batch([2 * page - 3], [min(new, 2 * page - 4)], 4, Hkv, D, page, seed=23, spare=0)
+        small = Batch([2 * page - 3], [new], heads, Hkv, D, page, seed=23, spare=0)
         bufs = []
         for i in range(2):
             x = torch.from_numpy(small.values[i]).to(torch.bfloat16)
@@ -345,24 +352,24 @@ def graph_of(f):
 
 
 def test_captured_and_replayed_with_other_tables():
-    """Two graphs of different shapes, each with its workspace; lengths, pages and rows change between the replays, eager calls run in between."""
+    """Three graphs of different shapes, each with its workspace, which lives as long as the graph; lengths, pages and rows change between the replays, eager calls run in between."""
     cases = []
-    for lengths, new, Hq, Hkv, seed in (([900, 400, 700], [1, 1, 1], 8, 2, 25), ([600, 800], [70, 60], 4, 2, 26)):
+    for lengths, new, Hq, Hkv, seed in (([900, 400, 700], [1, 1, 1], 8, 2, 25), ([600, 800], [70, 60], 4, 2, 26), ([1900, 800], [7, 9], 66, 2, 27)):
         b = Batch(lengths, new, Hq, Hkv, 128, 16, seed=seed)
         d = b.desc()
         dev = dict(q=b.q.cuda(), out=torch.zeros((b.T, Hq, 128), dtype=torch.bfloat16, device="cuda"), seq_rows=b.seq_rows.cuda(), lengths=torch.tensor(lengths, dtype=torch.int32).cuda(), table=b.table.cuda())
         ws = torch.zeros(max(1, B.axe_cache_attention_workspace(d)), dtype=torch.int32, device="cuda")
         run = lambda b=b, d=d, dev=dev, ws=ws: B.axe_cache_attention(d, dev["q"], b.kv[0], b.kv[1], dev["seq_rows"], dev["lengths"], dev["table"], dev["out"], workspace=ws)  # noqa: E731
-        cases.append((b, dev, graph_of(run)))
+        cases.append((b, dev, graph_of(run), ws))
     for turn in range(4):
-        for b, dev, g in cases:
+        for b, dev, g, _ in cases:
             lengths = [max(1, n - 137 * turn) for n in b.lengths]
             table = b.table.roll(turn, 1)
             dev["lengths"].copy_(torch.tensor(lengths, dtype=torch.int32))
             dev["table"].copy_(table)
             g.replay()
         torch.cuda.synchronize()
-        for b, dev, g in cases:
+        for b, dev, g, _ in cases:
             lengths = [max(1, n - 137 * turn) for n in b.lengths]
             table = b.table.roll(turn, 1)
             eager = b.run(lengths=torch.tensor(lengths, dtype=torch.int32), table=table)
@@ -371,13 +378,13 @@ def test_captured_and_replayed_with_other_tables():
 
 
 def test_two_calls_on_two_streams():
-    a, b = Batch([3000, 500], [1, 1], 8, 2, 128, 16, seed=27), Batch([700, 900], [100, 50], 8, 2, 128, 16, seed=28)
+    a, b = Batch([3000, 500], [1, 1], 8, 2, 128, 16, seed=27), Batch([700, 2900], [20, 10], 66, 2, 128, 16, seed=28)
     alone = [x.run() for x in (a, b)]
     streams = [torch.cuda.Stream() for _ in range(2)]
     sets = []
     for x in (a, b):
         d = x.desc()
-        sets.append((d, x.q.cuda(), x.seq_rows.cuda(), torch.tensor(x.lengths, dtype=torch.int32).cuda(), x.table.cuda(), torch.zeros((x.T, 8, 128), dtype=torch.bfloat16, device="cuda"),
+        sets.append((d, x.q.cuda(), x.seq_rows.cuda(), torch.tensor(x.lengths, dtype=torch.int32).cuda(), x.table.cuda(), torch.zeros((x.T, x.Hq, 128), dtype=torch.bfloat16, device="cuda"),
                      torch.zeros(max(1, B.axe_cache_attention_workspace(d)), dtype=torch.int32, device="cuda")))
     torch.cuda.synchronize()
     for _ in range(10):
