@@ -1002,22 +1002,18 @@ struct Attention {
       it.q = {__builtin_amdgcn_readlane(mine.row0, it.s), __builtin_amdgcn_readlane(mine.n, it.s), __builtin_amdgcn_readlane(mine.first, it.s), __builtin_amdgcn_readlane(mine.len, it.s)};
       t = (int)at - __builtin_amdgcn_readlane(upto, it.s);
     } else {
-      int64_t carry = 0;
-      if (threadIdx.x == 0) sh.found[0] = -1;
-      for (int base = 0; base < a.S; base += 256) {                // sequences from the last on
-        const int s = a.S - 1 - base - (int)threadIdx.x;
-        const int n = s >= 0 ? tiles_of(a, sequence(a, s), tokens) : 0;
-        int64_t total;
-        const int64_t before = carry + scan(n, total);
-        if (want >= before && want < before + n) sh.found[0] = s, sh.found[1] = n - 1 - (want - before);
-        carry += total;
-        lds_barrier();
-        if (want < carry) break;
-      }
-      lds_barrier();
-      it.s = __builtin_amdgcn_readfirstlane((int)sh.found[0]), t = __builtin_amdgcn_readfirstlane((int)sh.found[1]);
-      if (it.s < 0) return;
-      it.q = sequence(a, it.s);
+      // Places are counted so that a sequence's first follows from its first row alone: rows / tokens + the sequences before.  One place of a sequence may have no tile.
+      const int64_t at = a.T / tokens + a.S - 1 - want;
+      auto first_place = [&](int s) __attribute__((always_inline)) {
+        const int row = a.seq_rows[s];
+        return (int64_t)((uint32_t)(row < 0 ? 0 : row < a.T ? row : (int)a.T) / (uint32_t)tokens) + s;
+      };
+      const int s = at < 0 ? a.S : ended(a.S, [&](int i) __attribute__((always_inline)) { return first_place(i + 1) <= at; });
+      if (s >= a.S) return;
+      it.s = s, it.q = sequence(a, s);
+      const int64_t place = at - first_place(s);
+      if (place < 0 || place >= tiles_of(a, it.q, tokens)) return;
+      t = __builtin_amdgcn_readfirstlane((int)place);
     }
     tile(t, tokens);
     const Blocks b = blocks_of(it.keys);

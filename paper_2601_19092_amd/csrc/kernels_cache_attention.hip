@@ -108,7 +108,7 @@ hipError_t launch_cache_attention(const CacheArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   const int tokens = a.tile_rows / (int)a.group.d;
-  const int64_t tiles = (a.T / tokens + (a.S < a.T ? a.S : a.T)) * a.kv_heads;   // as many as there can be
+  const int64_t tiles = (a.T / tokens + (a.S < a.T || a.S > 64 ? a.S : a.T)) * a.kv_heads;   // as many as there can be; places, where there are more than 64 sequences
   constexpr int64_t kPiece = int64_t(1) << 23;                     // (a launch holds fewer than 2^32 threads)
   CacheArgs piece = a;
   for (piece.t0 = 0; piece.t0 < tiles; piece.t0 += kPiece) {

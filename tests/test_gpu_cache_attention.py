@@ -319,6 +319,11 @@ def test_more_sequences_than_a_workgroup_surveys():
     S = 4200
     b = Batch([3 + s % 40 for s in range(S)], [s % 3 for s in range(S)], 2, 1, 16, 16, seed=21, spare=0)
     b.check(b.run())
+    b = Batch([3 + s % 40 for s in range(300)], [max(0, s % 8 - 3) for s in range(300)], 4, 1, 64, 16, seed=22, spare=0)   # tiles of 16 rows, most sequences with one or none
+    b.check(b.run())
+    rows = b.seq_rows.clone()                                          # a padded batch: the last 100 sequences' rows are nobody's
+    rows[201:] = rows[200]
+    b.check(b.run(seq_rows=rows), seq_rows=rows)
 
 
 def test_a_cache_past_2_to_the_31_bytes():
