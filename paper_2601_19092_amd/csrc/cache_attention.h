@@ -347,7 +347,7 @@ struct Attention {
       return;
     }
     int ln = lane, page, slot;
-    if (a.reach31 && f.first >= it.keys.lo && f.first + 16 <= it.keys.hi) {   // all there, in pages of their own, and 32 bits hold the way to each: a lane works it out for each key
+    if (RT > 0 && a.reach31 && f.first >= it.keys.lo && f.first + 16 <= it.keys.hi) {   // all there, in pages of their own, and 32 bits hold the way to each: a lane works it out for each key (wide: bring_apart)
       asm volatile("" : "+v"(ln));
       const bool on = where(f.first + (ln & 15), page, slot);
       if (__all(on)) {
@@ -370,6 +370,29 @@ struct Attention {
       if (any && where(f.first + row, page, slot) && c < a.D * EB) from = cache + (page * pl.page + slot * pl.slot) * EB + c;
       load_lds<false>(from, lds + i * 1024);
     }
+  }
+  // Sixteen keys, K and V, that are all there, in pages of their own, where 32 bits hold the way to each: where they lie is worked out once.
+  // (Pages of 24, us, before / now: prompts and single tokens of 24 sequences, 16 heads of 64 columns, window 1000, 48 / 43; 4 x 512 over 8192 keys 343 / 314.  Worked out a block ahead: no faster.)
+  __device__ __forceinline__ bool bring_apart(int first, uint32_t k_lds, uint32_t v_lds) {
+    if (!a.reach31 || first < it.keys.lo || first + 16 > it.keys.hi) return false;
+    int ln = lane, page, slot;
+    asm volatile("" : "+v"(ln));
+    const bool on = where(first + (ln & 15), page, slot);
+    if (!__all(on)) return false;
+    const uint32_t k_at = (uint32_t)page * (uint32_t)(a.kp.page * 2) + (uint32_t)slot * (uint32_t)(a.kp.slot * 2);
+    const uint32_t v_at = (uint32_t)page * (uint32_t)(a.vp.page * 2) + (uint32_t)slot * (uint32_t)(a.vp.slot * 2);
+    const uint8_t *kb = (const uint8_t*)a.k_cache + (int64_t)it.head * a.kp.head * 2, *vb = (const uint8_t*)a.v_cache + (int64_t)it.head * a.vp.head * 2;
+    const bool alike = a.kp.page == a.vp.page && a.kp.slot == a.vp.slot;
+#pragma unroll
+    for (int i = 0; i < S2::NI; ++i) {
+      const int row = i * S2::RPI + ln / S2::CH, kc = (ln % S2::CH ^ S2::k(row)) * 16, vc = (ln % S2::CH ^ S2::v(row)) * 16;
+      const uint32_t k = (uint32_t)__shfl((int)k_at, row);
+      uint32_t v = k;
+      if (!alike) v = (uint32_t)__shfl((int)v_at, row);
+      if (kc < a.D * 2) load_lds<false>(k + kc, kb, k_lds + i * 1024);
+      if (vc < a.D * 2) load_lds<false>(v + vc, vb, v_lds + i * 1024);
+    }
+    return true;
   }
   // Which of KEYS keys there are.
   template <int KEYS>
@@ -403,11 +426,19 @@ struct Attention {
     const int first = block * kAttnKeys + wave * 16;
     need_pages(first, 16);
     const Found f = find(first);
-    const uint32_t there = f.side_by_side ? 0xffff : which<16>(first);
+    uint32_t there = 0xffff;
     if constexpr (!FP8) {
-      bring<2>(false, f, 0, lds_at(&sh.kv[stage][0][wave * 16 * ROW]));
-      bring<2>(true, f, 0, lds_at(&sh.kv[stage][1][wave * 16 * ROW]));
+      const uint32_t k_lds = lds_at(&sh.kv[stage][0][wave * 16 * ROW]), v_lds = lds_at(&sh.kv[stage][1][wave * 16 * ROW]);
+      if (f.side_by_side) {
+        bring<2>(false, f, 0, k_lds);
+        bring<2>(true, f, 0, v_lds);
+      } else if (!bring_apart(first, k_lds, v_lds)) {
+        there = which<16>(first);
+        bring<2>(false, f, 0, k_lds);
+        bring<2>(true, f, 0, v_lds);
+      }
     } else {
+      if (!f.side_by_side) there = which<16>(first);
       const uint8_t *kb = (const uint8_t*)a.k_cache + it.head * a.kp.head, *vb = (const uint8_t*)a.v_cache + it.head * a.vp.head;
       int64_t at = 0;                                              // of the scales: lane i brings those of key i
       bool on = true;

@@ -345,6 +345,21 @@ def test_a_cache_past_2_to_the_31_bytes():
         torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("page", [16, 24])
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("new, heads", [([1, 1], (4, 2)), ([9, 40], (4, 2)), ([9, 40], WIDE)])
+def test_keys_and_values_laid_out_differently(new, heads, cache, page):
+    b = Batch([900, 333], new, *heads, 128, page, "bf16", cache, seed=31)
+    shape, step = (b.pages, page, heads[1], 128), page * 144                # values: head by head, then by pages, 16 elements between neighbouring tokens
+    strides = (step, 144, b.pages * step, 1)
+    x = torch.as_strided(b.kv[1].view(torch.uint8) if cache == "fp8" else b.kv[1], shape, b.strides, 16)
+    buf = torch.zeros(heads[1] * b.pages * step, dtype=x.dtype, device="cuda")
+    torch.as_strided(buf, shape, strides).copy_(x)
+    b.kv[1] = buf.view(b.kv[1].dtype)
+    other = B.Layout(W.spec([(n, s, "m") for n, s in zip(shape, strides)]), ["m"])
+    b.check(b.run(desc=B.CacheDesc(b.T, 2, *heads, 128, b.pages, page, b.most, CODE["bf16"], CODE[cache], k_cache=b.layout, v_cache=other)))
+
+
 def graph_of(f):
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
