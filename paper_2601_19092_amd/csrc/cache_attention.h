@@ -13,6 +13,11 @@
 // Where a batch has few tiles, the list of all (tile, block of keys) is cut into as many equal runs as there are workgroups, wherever that falls; a tile that is cut leaves partial
 // results (maximum, sum, O) in the workspace, and a second kernel joins them, in the order of the keys.  Which run a workgroup has follows from the lengths alone: results repeat
 // their bits.
+//
+// Tiles of 16 and 32 rows, for sequences with few new tokens, are bound by memory: every wave has keys and LDS for itself, two turns of loads under way.  One token of each of 64 sequences up to 8192
+// tokens, 32 heads over 4 of 128 columns: 606 MB in 111 us, 5.5 TB/s; one of 131072, fp16: 537 MB in 97 us.  Wide tiles are bound by the matrix and the vector unit, which overlap in part: a prompt of 4096 tokens, 32 heads
+// over 8, 137 GFLOP in 147 - 150 us; matrix instructions and LDS reads alone 113, the terms and maxima alone 71, without the loads 146; one workgroup a compute unit in place of two 234.  4 x 512 over 8192 keys: 266
+// GFLOP in 274 - 278 us.
 #pragma once
 #include <hip/hip_runtime.h>
 
