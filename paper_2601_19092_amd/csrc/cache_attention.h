@@ -443,7 +443,6 @@ struct Attention {
         bring<2>(true, f, 0, v_lds);
       }
     } else {
-      if (!f.side_by_side) there = which<16>(first);
       const uint8_t *kb = (const uint8_t*)a.k_cache + it.head * a.kp.head, *vb = (const uint8_t*)a.v_cache + it.head * a.vp.head;
       int64_t at = 0;                                              // of the scales: lane i brings those of key i
       bool on = true;
@@ -460,16 +459,30 @@ struct Attention {
       } else {
         int ln = lane, page, slot;
         asm volatile("" : "+v"(ln));
-#pragma unroll
-        for (int i = 0; i < S2::NI; ++i) {
-          const int row = i * S2::RPI + ln / S2::CH, kc = (ln % S2::CH ^ S2::k(row)) * 8, vc = (ln % S2::CH ^ S2::v(row)) * 8;
-          const bool is = where(first + row, page, slot);
-          kreg[i] = vreg[i] = u32x2{};
-          if (is && kc < a.D) kreg[i] = *(const u32x2*)(kb + page * a.kp.page + slot * a.kp.slot + kc);
-          if (is && vc < a.D) vreg[i] = *(const u32x2*)(vb + page * a.vp.page + slot * a.vp.slot + vc);
-        }
         on = where(first + (ln & 15), page, slot);
+        there = (uint32_t)__ballot(on) & 0xffff;
         at = (int64_t)page * a.page.d + slot;
+        if (a.reach31 && there == 0xffff) {                        // (as bring_apart; a prompt of 1300 tokens, 20 heads over 5 of 80 columns, pages of 7, 67 -> 56 us; 8 x 1100, 24 over 3 of 192, pages of 100, 667 -> 524)
+          const uint32_t k_at = (uint32_t)page * (uint32_t)a.kp.page + (uint32_t)slot * (uint32_t)a.kp.slot, v_at = (uint32_t)page * (uint32_t)a.vp.page + (uint32_t)slot * (uint32_t)a.vp.slot;
+#pragma unroll
+          for (int i = 0; i < S2::NI; ++i) {
+            const int row = i * S2::RPI + ln / S2::CH, kc = (ln % S2::CH ^ S2::k(row)) * 8, vc = (ln % S2::CH ^ S2::v(row)) * 8;
+            const uint32_t k = (uint32_t)__shfl((int)k_at, row), v = (uint32_t)__shfl((int)v_at, row);
+            kreg[i] = vreg[i] = u32x2{};
+            if (kc < a.D) kreg[i] = *(const u32x2*)(kb + (k + kc));
+            if (vc < a.D) vreg[i] = *(const u32x2*)(vb + (v + vc));
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < S2::NI; ++i) {
+            const int row = i * S2::RPI + ln / S2::CH, kc = (ln % S2::CH ^ S2::k(row)) * 8, vc = (ln % S2::CH ^ S2::v(row)) * 8;
+            int p2, s2;
+            const bool is = where(first + row, p2, s2);
+            kreg[i] = vreg[i] = u32x2{};
+            if (is && kc < a.D) kreg[i] = *(const u32x2*)(kb + p2 * a.kp.page + s2 * a.kp.slot + kc);
+            if (is && vc < a.D) vreg[i] = *(const u32x2*)(vb + p2 * a.vp.page + s2 * a.vp.slot + vc);
+          }
+        }
       }
       sreg[0] = sreg[1] = 0;
       if (on) sreg[0] = a.k_scales[at * a.kv_heads + it.head], sreg[1] = a.v_scales[at * a.kv_heads + it.head];
