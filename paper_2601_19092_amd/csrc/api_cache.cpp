@@ -93,12 +93,12 @@ int plan_cache(const axe_cache_desc_t* g, const char* fn, Uses u, CachePlan& p) 
   }
   return AXE_OK;
 }
-// (Where it lies until the thread's next call of this kind.)
+// (Where it lies until the thread's next call of this kind.)  What a call's strides have to be multiples of goes by the cache's type, so that is in the key too.
 int kept_cache_plan(const axe_cache_desc_t* g, const char* fn, Uses u, const CachePlan*& out) {
   static thread_local LastPlan<CachePlan> last[2];
   LastPlan<CachePlan>& mine = last[u.kv];
   PlanKey key;
-  for (int64_t v : {g->T, g->pages, (int64_t)g->q_heads, (int64_t)g->kv_heads, (int64_t)g->head_dim, (int64_t)g->page_tokens, (int64_t)g->mem_axis, (int64_t)(4 * u.q + 2 * u.kv + u.o), g->q_elems,
+  for (int64_t v : {g->T, g->pages, (int64_t)g->q_heads, (int64_t)g->kv_heads, (int64_t)g->head_dim, (int64_t)g->page_tokens, (int64_t)g->cache_dtype, (int64_t)g->mem_axis, (int64_t)(4 * u.q + 2 * u.kv + u.o), g->q_elems,
                     g->k_elems, g->v_elems, g->out_elems, g->k_cache_elems, g->v_cache_elems})
     key.put(v);
   const bool keyed = (!u.q || key_of_layout(g->q, key)) && (!u.kv || (key_of_layout(g->k, key) && key_of_layout(g->v, key))) && (!u.o || key_of_layout(g->out, key)) &&
