@@ -148,10 +148,9 @@ struct Seq {
   int len;                         // keys
 };
 __device__ __forceinline__ Seq sequence(const CacheArgs& a, int s) {
-  const int T = (int)a.T, b0 = a.seq_rows[s], b1 = a.seq_rows[s + 1], l = a.lengths[s];
+  const int end = border(a, a.seq_rows[s + 1]), l = a.lengths[s];
   Seq q;
-  q.row0 = b0 < 0 ? 0 : b0 > T ? T : b0;
-  const int end = b1 > T ? T : b1;
+  q.row0 = border(a, a.seq_rows[s]);
   q.n = end > q.row0 ? end - q.row0 : 0;
   const int length = l < 0 ? 0 : l;
   q.len = length < a.capacity ? length : a.capacity;
@@ -1054,8 +1053,7 @@ struct Attention {
       // Places are counted so that a sequence's first follows from its first row alone: rows / tokens + the sequences before.  One place of a sequence may have no tile.
       const int64_t at = a.T / tokens + a.S - 1 - want;
       auto first_place = [&](int s) __attribute__((always_inline)) {
-        const int row = a.seq_rows[s];
-        return (int64_t)((uint32_t)(row < 0 ? 0 : row < a.T ? row : (int)a.T) / (uint32_t)tokens) + s;
+        return (int64_t)((uint32_t)border(a, a.seq_rows[s]) / (uint32_t)tokens) + s;
       };
       const int s = at < 0 ? a.S : ended(a.S, [&](int i) __attribute__((always_inline)) { return first_place(i + 1) <= at; });
       if (s >= a.S) return;

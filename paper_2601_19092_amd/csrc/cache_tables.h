@@ -22,6 +22,8 @@ __device__ __forceinline__ int ended(int S, ENDS ends) {
   }
   return __builtin_amdgcn_readfirstlane(lo);
 }
+// What seq_rows says, as it is taken: from 0 to T.
+__device__ __forceinline__ int border(const CacheArgs& a, int row) { return row < 0 ? 0 : row < a.T ? row : (int)a.T; }
 // The sequence that row t belongs to; -1: it is behind them all.
 __device__ __forceinline__ int sequence_of(const int32_t* seq_rows, int S, int64_t t) {
   const int s = ended(S, [&](int i) __attribute__((always_inline)) { return seq_rows[i + 1] <= t; });

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheArgs a) {
   }
   const int s = sequence_of(a.seq_rows, a.S, t);
   if (s < 0) return;
-  const int64_t first = a.seq_rows[s], last = a.seq_rows[s + 1], p = a.lengths[s] - last + t;
+  const int64_t first = border(a, a.seq_rows[s]), last = border(a, a.seq_rows[s + 1]), p = a.lengths[s] - last + t;
   if (t < first || p < 0 || p >= a.capacity) return;               // no token, or one without a place
   const int pos = (int)p;
   const uint32_t in_table = quotient(pos, a.page);
