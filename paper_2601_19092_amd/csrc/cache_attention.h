@@ -88,12 +88,22 @@ __device__ __forceinline__ float add2(uint32_t two, float c) {
   if constexpr (TYPE == kBf16) return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3f803f80u), c, false);
   else return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, two), f16x2{(_Float16)1.0f, (_Float16)1.0f}, c, false);
 }
-// What a term p counts in the sum when the product with V has t = p v, v the scale of V's row, as `rounded`: rounded / v.  A key that has nearly all the weight then has V's row for its result, not that times
-// the error of one rounding.
-__device__ __forceinline__ float weight(float p, float t, float v, float rounded) {
+// What a term p counts in the sum when the product with V has t = p v / lift, v the scale of V's row, as `rounded`: rounded lift / v.  A key that has nearly all the weight then has V's row for its result, not
+// that times the error of one rounding.  Where t is below the type's smallest steps, or near them, `rounded` says nothing of p, which then counts as it is: what a key weighs is not for the size of its value to say.
+template <int TYPE>
+__device__ __forceinline__ float weight(float p, float t, float v, float rounded, float lift) {
+  constexpr float LEAST = TYPE == kBf16 ? 0x1p-100f : 0x1p-14f;       // (p is at most 2^15: 1 / v is in range)
   const float by = __builtin_amdgcn_rcpf(v);
-  return fabsf(v) >= 1e-30f && fabsf(v) <= 1e30f ? fmaf(rounded - t, by, p) : p;
+  return fabsf(t) >= LEAST && fabsf(v) <= 1e30f ? fmaf((rounded - t) * lift, by, p) : p;
 }
+// e4m3 values in fp16: terms times scales stay inside fp16's range, and above its smallest steps, by being divided by `lift`, a power of two (2^-90 to 2^126): for every row the one above the largest scale that
+// it has seen, however small or large that is.  (A scale that is no number has no say in it; a row that sees an infinite one is not finite, whatever it is divided by.)
+constexpr float kLeastLift = 0x1p-90f;
+__device__ __forceinline__ float lift_above(float most) {
+  const uint32_t up = (__float_as_uint(most) & 0x7f800000u) + 0x800000u;
+  return __uint_as_float(up < 0x7e800000u ? up : 0x7e800000u);
+}
+__device__ __forceinline__ float over_lift(float lift) { return __uint_as_float(0x7f000000u - __float_as_uint(lift)); }   // 1 / lift
 // v of the four lanes of a column (lane mod 16) joined.
 template <class OP>
 __device__ __forceinline__ float quarters(float v) {
@@ -421,7 +431,7 @@ struct Attention {
   int lo, hi;                                                      // keys that this lane's row sees
   int w_lo, w_hi;                                                  // that all of the wave's rows see
   bool rows_here;
-  float lift_v;                                                    // e4m3 values in fp16: what their scales are divided by, a power of two
+  float lift_v;                                                    // e4m3 values in fp16: what their scales are divided by (lift_above)
   u32x2 kreg[FP8 ? S2::NI : 1], vreg[FP8 ? S2::NI : 1];            // e4m3: a block on its way
   float sreg[2];
 
@@ -522,7 +532,7 @@ struct Attention {
     const int last = rows - 1 < wave * 32 + 31 ? rows - 1 : wave * 32 + 31;
     w_lo = seen(a, it.q, it.i0 + (int)quotient(last, a.group), it.i0 + (int)quotient(last, a.group)).lo;   // (both ends grow with the token)
     w_hi = seen(a, it.q, it.i0 + (int)quotient(rows_here ? wave * 32 : 0, a.group), it.i0 + (int)quotient(rows_here ? wave * 32 : 0, a.group)).hi;
-    m = -INFINITY, l = 0, lift_v = 1;
+    m = -INFINITY, l = 0, lift_v = kLeastLift;
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = f32x16{};
   }
@@ -585,17 +595,28 @@ struct Attention {
     }
     const float less = LIFT - (m == -INFINITY ? 0.0f : m);
     float by_v = 1;
-    if constexpr (FP8 && TYPE == kF16) {                           // as in run_narrow
-      const float sv = sh.scales[stage][1][lane], most = wave_all<Max>(fabsf(sv) <= 3.0e38f ? fabsf(sv) : 0.0f);
-      if (most > lift_v) {
-        const float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + 0x800000u), down = lift_v / to;
+    if constexpr (FP8 && TYPE == kF16) {
+      float most = 0;
+      if (masked) {                                                // (of the keys that the row sees)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const f32x4 sv = *(const f32x4*)&sh.scales[stage][1][t * 32 + r * 8 + h * 4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most = fmaxf(most, s[t][r * 4 + e] > -INFINITY ? fabsf(sv[e]) : 0.0f);
+          }
+        most = fmaxf(most, other_half(most));
+      } else most = wave_all<Max>(fabsf(sh.scales[stage][1][lane]));
+      if (__any(most >= lift_v)) {
+        const float to = fmaxf(lift_v, lift_above(most)), down = lift_v / to;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[t][r] *= down;
         lift_v = to;
       }
-      by_v = 1.0f / lift_v;
+      by_v = over_lift(lift_v);
     }
     // lane i of 16 points at 4 columns of key i / 4 and receives 4 keys of column i
     const int i = lane & 15, row = h * 4 + (i >> 2);
@@ -758,7 +779,9 @@ struct Attention {
     }
     // keys that all rows see
     const int all_lo = seen(a, it.q, it.i0 + it.tokens - 1, it.i0 + it.tokens - 1).lo, all_hi = seen(a, it.q, it.i0, it.i0).hi;
-    float lift = 1;
+    float lift[RT];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) lift[x] = kLeastLift;
     clear_lds();
     uint32_t there[2];
     Found place[2][N];
@@ -821,22 +844,19 @@ struct Attention {
 #pragma unroll
           for (int x = 0; x < RT; ++x) s[x][n] *= ks;
         }
-        if constexpr (TYPE == kF16) {                              // terms times scales stay in fp16's range: the scales relative to a power of two that the largest so far is below
-          const float mine = sc[32 + (lane & 31)], most = wave_all<Max>(fabsf(mine) <= 3.0e38f ? fabsf(mine) : 0.0f);
-          if (most > lift) {
-            const float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + 0x800000u), down = lift / to;
-#pragma unroll
-            for (int x = 0; x < RT; ++x)
-#pragma unroll
-              for (int t = 0; t < DN; ++t) on[x][t] *= down;
-            lift = to;
-          }
-        }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // K is read: its place is free
       issue_k(ahead, turn);
       const bool masked = is != (N == 2 ? 0xffffffffu : 0xffffu) || first < all_lo || first + KT > all_hi;
       s16x8 pk[RT];
+      float of_all = 0;
+      if constexpr (FP8 && TYPE == kF16) {
+        if (!masked) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) of_all = fmaxf(of_all, fabsf(vs[e >> 2][e & 3]));
+          of_all = quarters<Max>(of_all);
+        }
+      }
 #pragma unroll
       for (int x = 0; x < RT; ++x) {
         if (masked) {
@@ -863,12 +883,28 @@ struct Attention {
         for (int e = 0; e < 4 * N; ++e) p[e] = exp2_fast(fmaf(s[x][e >> 2][e & 3], a.scale_log2, less));
         u32x4 w = {};
         if constexpr (FP8) {
-          const float by = 1.0f / lift;
+          float by = 1, over = 1;
+          if constexpr (TYPE == kF16) {
+            float most = of_all;
+            if (masked) {                                          // (of the keys that the row sees)
+              most = 0;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) most = fmaxf(most, s[x][e >> 2][e & 3] > -INFINITY ? fabsf(vs[e >> 2][e & 3]) : 0.0f);
+              most = quarters<Max>(most);
+            }
+            if (__any(most >= lift[x])) {
+              const float to = fmaxf(lift[x], lift_above(most)), down = lift[x] / to;
+#pragma unroll
+              for (int t = 0; t < DN; ++t) on[x][t] *= down;
+              lift[x] = to;
+            }
+            over = lift[x], by = over_lift(over);
+          }
 #pragma unroll
           for (int e = 0; e < 8; e += 2) {
-            const float v0 = vs[e >> 2][e & 3] * by, v1 = vs[e >> 2][e & 3 | 1] * by, t0 = p[e] * v0, t1 = p[e + 1] * v1;
+            const float v0 = vs[e >> 2][e & 3], v1 = vs[e >> 2][e & 3 | 1], t0 = p[e] * by * v0, t1 = p[e + 1] * by * v1;
             w[e >> 1] = pack2<TYPE>(t0, t1);
-            ls[x] += weight(p[e], t0, v0, half<TYPE>(w[e >> 1], 0)) + weight(p[e + 1], t1, v1, half<TYPE>(w[e >> 1], 1));
+            ls[x] += weight<TYPE>(p[e], t0, v0, half<TYPE>(w[e >> 1], 0), over) + weight<TYPE>(p[e + 1], t1, v1, half<TYPE>(w[e >> 1], 1), over);
           }
         } else {
 #pragma unroll
@@ -939,7 +975,7 @@ struct Attention {
       const int r = x * 16 + col;
       if (kg == 0) sh.top[wave][r] = mx[x], sh.sum[wave][r] = ls[x];
 #pragma unroll
-      for (int t = 0; t < DN; ++t) *(f32x4*)(mine + r * DP + ((t * 4 + kg) ^ (r & 7)) * 4) = on[x][t] * lift;
+      for (int t = 0; t < DN; ++t) *(f32x4*)(mine + r * DP + ((t * 4 + kg) ^ (r & 7)) * 4) = FP8 && TYPE == kF16 ? on[x][t] * lift[x] : on[x][t];
     }
     lds_barrier();
     constexpr int PER = DP / 64;                                   // f32x4 of a thread: 16 threads a row
