@@ -117,6 +117,14 @@ __device__ __forceinline__ float other_half(float v) {              // of lane ^
   return __int_as_float((threadIdx.x & 32) ? s[0] : s[1]);
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// The terms are exp2(s by + less), by = scale / ln 2 and less = LIFT - m, m the row's maximum: one instruction, which does not round the product s by as m was rounded.  What that leaves between the largest score and
+// m is nothing beside LIFT as long as m is small (2^-4 at this size), and out of the terms' range when it is not (fp16 from 2^28 on).  There the scores become s by, rounded, less m first.
+constexpr float kLargeScore = 0x1p20f;
+__device__ __forceinline__ float less_maximum(float s, float by, float m) {
+  float x = s * by;
+  asm volatile("" : "+v"(x));                                       // (rounded here)
+  return x - m;
+}
 
 // 16 bytes that are zero: what a lane brings to LDS for a key that is not there.
 __device__ const u32x4 kNothing = {0, 0, 0, 0};
@@ -593,7 +601,13 @@ struct Attention {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] *= by;
     }
-    const float less = LIFT - (m == -INFINITY ? 0.0f : m);
+    const float base = m == -INFINITY ? 0.0f : m;
+    float less = LIFT - base, by_s = a.scale_log2;
+    if (__builtin_expect(__any(fabsf(base) > kLargeScore), 0)) {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) s[r >> 4][r & 15] = less_maximum(s[r >> 4][r & 15], by_s, base);
+      less = LIFT, by_s = 1;
+    }
     float by_v = 1;
     if constexpr (FP8 && TYPE == kF16) {
       float most = 0;
@@ -630,7 +644,7 @@ struct Attention {
     u32x4 p[4];
     auto two = [&](int k, int e) __attribute__((always_inline)) {
       const int r = (k & 1) * 8 + 2 * e;
-      const float x = exp2_fast(fmaf(s[k >> 1][r], a.scale_log2, less)), y = exp2_fast(fmaf(s[k >> 1][r + 1], a.scale_log2, less));
+      const float x = exp2_fast(fmaf(s[k >> 1][r], by_s, less)), y = exp2_fast(fmaf(s[k >> 1][r + 1], by_s, less));
       if constexpr (FP8) {
         const float* sc = &sh.scales[stage][1][k * 16 + (e >> 1) * 8 + h * 4 + (e & 1) * 2];
         const float v0 = sc[0] * by_v, v1 = sc[1] * by_v, t0 = x * v0, t1 = y * v1;
@@ -877,10 +891,16 @@ struct Attention {
 #pragma unroll
           for (int t = 0; t < DN; ++t) on[x][t] *= by;
         }
-        const float less = LIFT - (mx[x] == -INFINITY ? 0.0f : mx[x]);
+        const float base = mx[x] == -INFINITY ? 0.0f : mx[x];
+        float less = LIFT - base, by_s = a.scale_log2;
+        if (__builtin_expect(__any(fabsf(base) > kLargeScore), 0)) {
+#pragma unroll
+          for (int e = 0; e < 4 * N; ++e) s[x][e >> 2][e & 3] = less_maximum(s[x][e >> 2][e & 3], by_s, base);
+          less = LIFT, by_s = 1;
+        }
         float p[4 * N];
 #pragma unroll
-        for (int e = 0; e < 4 * N; ++e) p[e] = exp2_fast(fmaf(s[x][e >> 2][e & 3], a.scale_log2, less));
+        for (int e = 0; e < 4 * N; ++e) p[e] = exp2_fast(fmaf(s[x][e >> 2][e & 3], by_s, less));
         u32x4 w = {};
         if constexpr (FP8) {
           float by = 1, over = 1;
