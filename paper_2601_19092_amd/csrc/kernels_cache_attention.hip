@@ -32,14 +32,15 @@ struct Join {
           const float* p = a.ws + part_at(a, group + at, at == 0, DP) + 4;
 #pragma unroll
           for (int i = 0; i < RB; ++i) {
-            pm[i][k] = j < n ? p[row[i]] : -INFINITY, pl[i][k] = p[a.ws_rows + row[i]];
+            pm[i][k] = p[row[i]], pl[i][k] = p[a.ws_rows + row[i]];
             v[i][k] = *(const f32x4*)(p + 2 * a.ws_rows + (int64_t)row[i] * DP + c);
           }
         }
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
-          for (int k = 0; k < DEPTH; ++k) add(top[i], l[i], o[i], pm[i][k], pl[i][k], v[i][k]);
+          for (int k = 0; k < DEPTH; ++k)
+            if (j0 + k * AT_ONCE < n) add(top[i], l[i], o[i], pm[i][k], pl[i][k], v[i][k]);
       }
 #pragma unroll
       for (int i = 0; i < RB; ++i) {
@@ -52,11 +53,10 @@ struct Join {
       }
     }
   }
-  // Two results of one row (a maximum of -inf: no key was seen, and the rest is 0).
+  // Two results of one row.  (A maximum of -inf: no key was seen, and the rest is 0, or none of the scores was a number, and it is NaN, which stays.)
   static __device__ __forceinline__ void add(float& top, float& l, f32x4& o, float pm, float pl, f32x4 v) {
     const float t = fmaxf(top, pm), base = t == -INFINITY ? 0.0f : t, old = exp2_fast(top - base), by = exp2_fast(pm - base);
-    top = t, l = l * old, o = o * old;
-    if (pm != -INFINITY) l += pl * by, o += v * by;
+    top = t, l = l * old + pl * by, o = o * old + v * by;
   }
   template <int FAR>
   static __device__ __forceinline__ void other(float& top, float& l, f32x4& o) {
