@@ -32,15 +32,17 @@ struct Join {
           const float* p = a.ws + part_at(a, group + at, at == 0, DP) + 4;
 #pragma unroll
           for (int i = 0; i < RB; ++i) {
-            pm[i][k] = p[row[i]], pl[i][k] = p[a.ws_rows + row[i]];
+            pm[i][k] = j < n ? p[row[i]] : -INFINITY, pl[i][k] = p[a.ws_rows + row[i]];
             v[i][k] = *(const f32x4*)(p + 2 * a.ws_rows + (int64_t)row[i] * DP + c);
           }
         }
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
-          for (int k = 0; k < DEPTH; ++k)
-            if (j0 + k * AT_ONCE < n) add(top[i], l[i], o[i], pm[i][k], pl[i][k], v[i][k]);
+          for (int k = 0; k < DEPTH; ++k) {
+            const bool there = j0 + k * AT_ONCE < n;
+            add(top[i], l[i], o[i], pm[i][k], there ? pl[i][k] : 0.0f, there ? v[i][k] : f32x4{});
+          }
       }
 #pragma unroll
       for (int i = 0; i < RB; ++i) {
