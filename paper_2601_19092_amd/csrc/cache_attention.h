@@ -279,6 +279,7 @@ struct Attention {
     float top[4][32], sum[4][32];                                  // narrow: the waves' maxima and sums
     uint16_t there[2][4];                                          // wide: of a wave's 16 keys: which there are
     int flags[4];
+    uint8_t marks[kAttnRows];                                      // of a tile's tokens, see survey
     int64_t sums[8];
     int64_t found[4];
   };
@@ -717,8 +718,9 @@ struct Attention {
     return x;
   }
 
-  // The item's result: part < 0: to out; else a partial result, of which these are the tokens from `skip` on.
-  __device__ __forceinline__ void finish_wide(int group, int part, int ends, int skip, int of) {
+  // The item's result: part < 0: to out; else a partial result, of all of the tile's tokens or of some (see work).
+  __device__ __forceinline__ void finish_wide(int group, int part, int ends, uint32_t once_more) {
+    const int skip = once_more & 255, of = once_more ? once_more >> 8 : it.tokens;
     const int G = a.group.d, r = wave * 32 + (lane & 31), rows = it.tokens * G;
     const bool on = r < rows;
     if (part < 0) {
@@ -754,7 +756,7 @@ struct Attention {
 
   // Every wave has all rows, and keys of its own: KT of every 4 KT.  They come into its own LDS, K and V each two turns ahead, waited for by count: no barrier, and as soon as a
   // turn's K is read the next but one is on its way.  What the waves have is joined at the end.  (Where keys are read for few rows, memory is what bounds; the loads under way are what counts.)
-  __device__ __forceinline__ void run_narrow(int group, int part, int ends, int skip, int of, bool check, bool& again) {
+  __device__ __forceinline__ void run_narrow(int group, int part, int ends, uint32_t once_more, bool& again) {
     constexpr int N = KT / 16, DN = DP / 16, SN32 = DP / 32;
     constexpr int LK = N * SN::NI + (FP8 ? 1 : 0), LV = N * SN::NI;  // loads of a turn
     const int G = a.group.d, col = lane & 15, kg = lane >> 4, rows = it.tokens * G;
@@ -985,9 +987,9 @@ struct Attention {
 #pragma unroll
         for (int e = 0; e < 4; ++e) bad = fmaf(on[x][t][e], 0.0f, bad);
     }
-    again = check && not_finite(bad);
+    again = checked(once_more) && not_finite(bad);
+    const int skip = once_more & 255, of = once_more ? once_more >> 8 : it.tokens;
     lds_barrier();                                                 // (the turns are free)
-    if (again) return;
     // the waves' results, 16 bytes changing places by the row
     float* mine = (float*)&sh.kv[0][0][0] + wave * (RT * 16 * DP);
 #pragma unroll
@@ -1037,24 +1039,91 @@ struct Attention {
   }
 
   // Values of keys that some rows of a tile see and others do not: the product has them in all rows, times 0, which is not 0 if they are not finite.  So where something that is not finite has come
-  // out, the tokens are done one by one: a token's rows see the same keys, and the others are zeros in LDS.
+  // out, such keys are looked at: at token i of the tile one may come into sight (its own) and, with a window, one go out of sight.  marks[i]: kEnters, kLeaves: that one's value is not finite; kEntersNaN,
+  // kLeavesNaN: and nothing but NaN, so that the tokens which see it need no second pass.
+  static constexpr uint32_t kEnters = 1, kLeaves = 2, kEntersNaN = 4, kLeavesNaN = 8;
+  __device__ __forceinline__ void survey() {
+    const int first = it.q.first + it.i0;                          // position of the first token
+    const int from = it.keys.lo > it.b0 * kAttnKeys ? it.keys.lo : it.b0 * kAttnKeys, end = it.keys.hi < it.b1 * kAttnKeys ? it.keys.hi : it.b1 * kAttnKeys;
+#pragma unroll 1
+    for (int i = wave; i < it.tokens; i += 4) {
+      uint32_t mark = 0;
+#pragma unroll 1
+      for (int leaves = 0; leaves < (a.window ? 2 : 1); ++leaves) {
+        const int key = leaves ? first + i - a.window : first + i;
+        if (key < from || key >= end) continue;
+        const int p = (int)quotient(key, a.page), page = a.table[(int64_t)it.s * a.max_pages + p], slot = key - p * (int)a.page.d;
+        if ((uint32_t)page >= (uint64_t)a.pages) continue;
+        constexpr int EB = FP8 ? 1 : 2;
+        const bool in = lane * 16 < a.D * EB;
+        u32x4 v = {};
+        if (in) v = load_bits<u32x4>((const uint8_t*)a.v_cache + (page * a.vp.page + slot * a.vp.slot + it.head * a.vp.head) * EB + lane * 16);
+        bool any = false, all = true;                              // not finite; NaN
+#pragma unroll
+        for (int k = 0; k < 16 / EB; ++k) {
+          const uint32_t x = v[k * EB / 4] >> (k * EB % 4 * 8) & (FP8 ? 0x7f : 0x7fff), top = FP8 ? 0x7f : TYPE == kBf16 ? 0x7f80 : 0x7c00;   // (e4m3: 0x7f is NaN, the rest is finite)
+          any |= x >= top, all &= FP8 ? x == top : x > top;
+        }
+        any = __any(any), all = __all(all || !in);
+        if constexpr (FP8) {
+          const float sc = a.v_scales[((int64_t)page * a.page.d + slot) * a.kv_heads + it.head];
+          any |= !(fabsf(sc) <= (TYPE == kF16 ? 0x1p30f : 3.4028234663852886e38f));   // (fp16: large enough, relative to others, to be an infinity on the way)
+          all |= sc != sc;
+        }
+        if (any) mark |= (kEnters | (all ? kEntersNaN : 0)) << leaves;
+      }
+      if (lane == 0) sh.marks[i] = (uint8_t)mark;
+    }
+    lds_barrier();
+  }
+  // Whether a bit from `from` up to `end` is set.
+  static __device__ __forceinline__ bool any_of(const uint64_t (&b)[2], int from, int end) {
+    auto below = [](int n) __attribute__((always_inline)) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
+    return (b[0] & below(end) & ~below(from)) | (b[1] & below(end - 64) & ~below(from - 64));
+  }
+  // The next of a tile's `tokens` from token `from` on, as many as see the same of the marked keys, that do not see one of them, unless they see one that is NaN all through: `first`, and how many; 0: no more.
+  __device__ __forceinline__ int spoilt(int tokens, int from, int& first) {
+    const uint32_t m0 = lane < tokens ? sh.marks[lane] : 0, m1 = 64 + lane < tokens ? sh.marks[64 + lane] : 0;
+    auto bits = [&](uint32_t kind, uint64_t (&b)[2]) __attribute__((always_inline)) { b[0] = __ballot((m0 & kind) != 0), b[1] = __ballot((m1 & kind) != 0); };
+    uint64_t enters[2], leaves[2], enters_nan[2], leaves_nan[2], changes[2];
+    bits(kEnters, enters), bits(kLeaves, leaves), bits(kEntersNaN, enters_nan), bits(kLeavesNaN, leaves_nan), bits(kEnters | kLeaves, changes);
+    const int window = a.window && a.window < tokens ? a.window : tokens;
+    int next;
+    for (first = from; first < tokens; first = next) {
+      for (next = first + 1; next < tokens && !any_of(changes, next, next + 1);) ++next;
+      const bool unseen = any_of(leaves, 0, first + 1) || any_of(enters, first + 1, tokens);
+      const bool lost = any_of(enters_nan, first - window + 1, first + 1) || any_of(leaves_nan, first + 1, first + window + 1);
+      if (unseen && !lost) return next - first;
+    }
+    return 0;
+  }
   __device__ __forceinline__ void work(int group, int part, int ends) {
-    const int i0 = it.i0, tokens = it.tokens;
-    for (int i = -1; i < tokens; ++i) {
-      if (i >= 0) it.i0 = i0 + i, it.tokens = 1, it.keys = seen(a, it.q, it.i0, it.i0);
-      const bool check = i < 0 && a.causal && tokens > 1;
-      const int skip = i < 0 ? 0 : i;
-      bool again = false;
-      if constexpr (RT > 0) run_narrow(group, part, ends, skip, tokens, check, again);
+    // 0: all of the tile's tokens; else some of them once more: how many the tile has, and the first of these.  (One register for the loop over the keys, which has none to spare.)
+    uint32_t once_more = 0;
+    for (bool again = false;;) {
+      if constexpr (RT > 0) run_narrow(group, part, ends, once_more, again);
       else {
         run_wide();
-        again = check && not_finite(check_wide());
+        again = checked(once_more) && not_finite(check_wide());
         lds_barrier();                                             // (the stages are free)
-        if (!again) finish_wide(group, part, ends, skip, tokens);
+        finish_wide(group, part, ends, once_more);
       }
-      if (i < 0 && !again) break;
+      if (__builtin_expect(!once_more && !again, 1)) return;
+      int skip = once_more & 255, n = it.tokens, first;
+      const int tokens = once_more ? once_more >> 8 : n;
+      if (!once_more) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (what is done again is written again, by other waves)
+        survey();
+        n = 0;
+      }
+      it.i0 -= skip;
+      n = __builtin_amdgcn_readfirstlane(spoilt(tokens, skip + n, first)), skip = __builtin_amdgcn_readfirstlane(first);
+      if (n == 0) return;
+      once_more = tokens << 8 | skip, it.i0 += skip, it.tokens = n, it.keys = seen(a, it.q, it.i0, it.i0 + n - 1);
     }
   }
+  // Whether the tokens see different keys, and it has not been looked at yet what those hold.
+  __device__ __forceinline__ bool checked(uint32_t once_more) const { return !once_more && a.causal && it.tokens > 1; }
 
   __device__ __forceinline__ void tile(int tile, int tokens) {
     it.i0 = tile * tokens;
