@@ -455,14 +455,16 @@ int axe_rows_combine_backward(const axe_rows_desc_t* g, const void* d_dtokens, c
  *   q_heads          : a multiple of kv_heads, at most 128 times as many; head h reads head h / (q_heads / kv_heads) of the cache.
  *   head_dim         : a multiple of 8, with an e4m3 cache of 16, up to 256.  T, max_pages page_tokens and pages up to 2^30, S below 2^20, heads below 2^16.
  *
- * axe_cache_append -- cache[s, p] = (rot_p(k), v), q_out = rot_p(q) for every new token.
+ * axe_cache_append -- cache[s, p] = (rot_p(k), v), q_out = rot_p(q) for every new token that has a place in the table (q_out of the others, as of rows that no sequence has, is left as it is).
  *   rot_p turns the first rotary_dim (even, up to head_dim, or 0) columns of a head in pairs, (a, b) -> (a cos - b sin, b cos + a sin): columns (i, i + rotary_dim / 2) (AXE_ROTATE_HALVES) or
  *   (2 i, 2 i + 1) (AXE_ROTATE_PAIRS), by the cosine [p][i] and the sine [p][rotary_dim / 2 + i] of d_rotation, (max_pages page_tokens, rotary_dim) fp32, contiguous.
  *   d_q and d_q_out (layouts q and out; q_out may be q with the same layout) are given together, or both NULL: keys and values alone.
  *   In 32 bits, rounded once.  e4m3: s = max(|row|) / 448 over the head's columns, at least 2^-126, 1 where all are 0; codes as axe_rmsnorm makes them.
  * axe_cache_attention -- out[t, h] = sum_j softmax_j(scale q[t, h] . K[j]) V[j] over the sequence's keys j < lengths[s] that the token at position p sees: causal: j <= p; window > 0 (causal
  *   only): j > p - window, the token itself among them; otherwise all.  A token that sees no key: zeros.  scale from 2^-100 to 2^100.  Masked keys and values have no part in the result, whatever they hold
- *   (NaN, infinities); a score of -inf counts as masked.  Scores, statistics and sums in 32 bits; the softmax's terms are rounded to dtype for the product with V.
+ *   (NaN, infinities).  A score of -inf is a weight of 0 (a token that has no other: zeros), which a value that is not finite makes NaN all the same.  Scores, statistics and sums in 32 bits; the softmax's
+ *   terms are rounded to dtype for the product with V: in fp16 what is below 2^-34 of a row's largest term (e4m3 cache: 2^-33 of that and the largest scale of V the row sees) is lost.
+ *   Values that are not finite where some of the new tokens see them and others do not cost time: up to a pass over the keys for each such value.
  *   d_ws, ws_elems : workspace of axe_cache_attention_workspace(g) 4-byte words (may be 0), owned by the caller, overwritten.
  * Both may be captured into a graph and replayed with other contents of the three arrays: launches depend on the descriptor alone. */
 enum { AXE_ROTATE_HALVES = 0, AXE_ROTATE_PAIRS = 1 };
