@@ -8,7 +8,8 @@
 //   S^T = K Q^T      a lane holds 32 of the 64 scores of one row, lane + 32 the others: maximum and sum of a row are a chain in the lane and one exchange;
 //   O^T += V^T P^T   the scores' registers, in 16 bits, are the product's operand as they are: its contraction runs over the keys in the order in which the registers hold them, and V comes out of LDS in
 //                    that order by transposing reads.
-// The maximum is a running one: when it grows, sums and O are multiplied down.  Everything but the products' operands is fp32.
+// The maximum is a running one: when it grows, sums and O are multiplied down.  Everything but the products' operands is fp32.  The terms are one of them: matrix instructions take 16-bit operands at 16 times the rate
+// of fp32 ones, and a term's rounding, 2^-8 or 2^-11 of it at most, is no larger than the result's own (relative error against 64 bits 2.0e-3 in bf16, 2.6e-4 in fp16; with terms in fp32 1.6e-3, 2.1e-4).
 //
 // Where a batch has few tiles, the list of all (tile, block of keys) is cut into as many equal runs as there are workgroups, wherever that falls; a tile that is cut leaves partial
 // results (maximum, sum, O) in the workspace, and a second kernel joins them, in the order of the keys.  Which run a workgroup has follows from the lengths alone: results repeat
@@ -16,8 +17,8 @@
 //
 // Tiles of 16 and 32 rows, for sequences with few new tokens, are bound by memory: every wave has keys and LDS for itself, two turns of loads under way.  One token of each of 64 sequences up to 8192
 // tokens, 32 heads over 4 of 128 columns: 606 MB in 111 us, 5.5 TB/s; one of 131072, fp16: 537 MB in 97 us.  Wide tiles are bound by the matrix and the vector unit, which overlap in part: a prompt of 4096 tokens, 32 heads
-// over 8, 137 GFLOP in 147 - 150 us; matrix instructions and LDS reads alone 113, the terms and maxima alone 71, without the loads 146; one workgroup a compute unit in place of two 234.  4 x 512 over 8192 keys: 266
-// GFLOP in 274 - 278 us.
+// over 8, 137 GFLOP in 148 - 157 us; matrix instructions and LDS reads alone 113, the terms and maxima alone 71, without the loads 146; one workgroup a compute unit in place of two 234.  4 x 512 over 8192 keys: 266
+// GFLOP in 270 - 288 us.
 #pragma once
 #include <hip/hip_runtime.h>
 

@@ -74,7 +74,11 @@ inline int attn_slots(int D) { return attn_columns(D) <= 128 ? 512 : 256; }
 // on average that a place on the chip is idle.  us, split / whole: 512 new tokens, 32 heads over 4, 39 / 18; 1024, 32 over 8, 51 / 29; 24 x 100 over 1100 keys, 16 heads of 64 columns, 56 / 32;
 // 256 over 2048 keys 42 / 75.  Narrow tiles, by the same: up to 768 keys, twice that where 64 tiles or more share the chip's bandwidth; one token, 32 heads over 4, of 512 keys 12.4 / 11.0, of 1024
 // 14.4 / 16.3; 16 tokens, 32 over 8, of 1536 27.3 / 25.2; 64 tokens of 1024 51.8 / 46.5.
-// Rows of a tile: as many as the sequences have on average, up to 32; from there on 128, or 32 where 128 would leave most of the chip without a tile.  us, 128 / 32 rows: 38 wide tiles, 600 new
+// The keys counted are those that the table has room for, not the lengths: these are the device's to know, and launches and the workspace follow from the descriptor alone.  So the same call is split under a table
+// of a server's longest sequence.  us, a table as wide as the longest sequence / one of 8192 pages: 512 new tokens, 32 heads over 4, 19.3 / 39.7; 1024, 32 over 8, 32.1 / 49.9; 24 x 100 over 1100 keys 36.5 / 52.8; one
+// token of 500 keys 12.2 / 13.5; 16 of 1000 19.4 / 22.0.
+// Rows of a tile: 128 where those alone fill the chip twice, or above 4096 sequences (one token of each of 512 sequences of 100 keys, 128 heads over 16 of 256 columns: 394 us, of 496, in tiles of 16, 404).  Else as many
+// as the sequences have on average, up to 32; from there on 128, or 32 where 128 would leave most of the chip without a tile.  us, 128 / 32 rows: 38 wide tiles, 600 new
 // tokens over 700 keys of 256 columns, 39 / 30; 32, 128 tokens over 8192, 77 / 69; 16, 64 over 2048, 36 / 34; 64, 256 over 2048, 42 / 49; 128, 100 of each of 8 over 2200, 54 / 79.
 struct AttnShape {
   int tile_rows, groups, ws_rows;
