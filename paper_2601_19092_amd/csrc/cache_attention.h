@@ -98,7 +98,8 @@ __device__ __forceinline__ float weight(float p, float t, float v, float rounded
   return fabsf(t) >= LEAST && fabsf(v) <= 1e30f ? fmaf((rounded - t) * lift, by, p) : p;
 }
 // e4m3 values in fp16: terms times scales stay inside fp16's range, and above its smallest steps, by being divided by `lift`, a power of two (2^-90 to 2^126): for every row the one above the largest scale that
-// it has seen, however small or large that is.  (A scale that is no number has no say in it; a row that sees an infinite one is not finite, whatever it is divided by.)
+// it has seen, however small or large that is.  (A scale that is no number has no say in it; a row that sees an infinite one is not finite, whatever it is divided by.  By the row
+// and not by the tile: 7 - 9 % of the time in tiles of 32 rows, 0 - 3 elsewhere.)
 constexpr float kLeastLift = 0x1p-90f;
 __device__ __forceinline__ float lift_above(float most) {
   const uint32_t up = (__float_as_uint(most) & 0x7f800000u) + 0x800000u;
@@ -1041,7 +1042,8 @@ struct Attention {
 
   // Values of keys that some rows of a tile see and others do not: the product has them in all rows, times 0, which is not 0 if they are not finite.  So where something that is not finite has come
   // out, such keys are looked at: at token i of the tile one may come into sight (its own) and, with a window, one go out of sight.  marks[i]: kEnters, kLeaves: that one's value is not finite; kEntersNaN,
-  // kLeavesNaN: and nothing but NaN, so that the tokens which see it need no second pass.
+  // kLeavesNaN: and nothing but NaN, so that the tokens which see it need no second pass.  (12000 keys under 128 tokens, 48 heads, us: 84; one value not finite 148, a query 150, all new values NaN 169.  All tokens
+  // one by one, as it was: 2100 - 4600.)
   static constexpr uint32_t kEnters = 1, kLeaves = 2, kEntersNaN = 4, kLeavesNaN = 8;
   __device__ __forceinline__ void survey() {
     const int first = it.q.first + it.i0;                          // position of the first token
